@@ -15,6 +15,7 @@ from typing import Optional
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcosa.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "cosa.h")
+DECODE_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "cosa_decode.h")
 
 COSA_OK, COSA_ERR_INVALID_ARG, COSA_ERR_UNSUPPORTED, COSA_ERR_WORKSPACE, COSA_ERR_HIP = range(5)
 SELECT_FRACTION, SELECT_TOP_P, SELECT_ALL = 0, 1, 2
@@ -58,6 +59,24 @@ class CosaVarlen(ctypes.Structure):
 MAX_PACKED_SEQS = 128
 
 
+class CosaDecodeProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("sm_scale", ctypes.c_float)]
+
+
+class CosaPageBudget(ctypes.Structure):
+    _fields_ = [("fraction", ctypes.c_float), ("min_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("sink_pages", ctypes.c_int32),
+                ("recent_pages", ctypes.c_int32)]
+
+
+class CosaDecodeSparseLayout(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_size_t), ("pages", ctypes.c_size_t), ("count", ctypes.c_size_t),
+                ("partial", ctypes.c_size_t), ("total", ctypes.c_size_t)]
+
+
 class CosaError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(message)
@@ -85,12 +104,29 @@ class Problem:
                            self.head_dim, self.block, self.stride, self.sm_scale, self.causal)
 
 
+@dataclass(frozen=True)
+class DecodeProblem:
+    """One new token for each sequence of a batch (cosa_decode_problem). q_stride 0: the queries are
+    dense, or a tensor passed as q brings its own stride."""
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    max_pages: int
+    head_dim: int = 128
+    q_stride: int = 0
+    sm_scale: float = 0.0
+
+    def c(self) -> CosaDecodeProblem:
+        return CosaDecodeProblem(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
+                                 self.max_pages, self.q_stride, self.sm_scale)
+
+
 _lib = None
 
 
-def declared_symbols():
-    """Names of the functions include/cosa.h declares."""
-    text = open(HEADER_PATH).read()
+def declared_symbols(header=None):
+    """Names of the functions a header declares (include/cosa.h by default)."""
+    text = open(header or HEADER_PATH).read()
     return sorted(set(re.findall(r"^\s*(?:const\s+)?[a-z_0-9]+\*?\s+\*?(cosa_[a-z_0-9]+)\(", text,
                                  re.M)))
 
@@ -173,6 +209,29 @@ def lib():
         L.cosa_prefill_paged_varlen.argtypes = [P, VL, vp, KV, ctypes.POINTER(CosaSelect),
                                                 ctypes.POINTER(CosaSkip), vp, ctypes.c_size_t, vp,
                                                 vp]
+        D, PB = ctypes.POINTER(CosaDecodeProblem), ctypes.POINTER(CosaPageBudget)
+        i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        L.cosa_page_map.restype = S
+        L.cosa_page_map.argtypes = [i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.cosa_kv_append.restype = S
+        L.cosa_kv_append.argtypes = [i32, i32, i32, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.cosa_page_score.restype = S
+        L.cosa_page_score.argtypes = [D, vp, KV, vp, vp, vp, vp]
+        L.cosa_page_select.restype = S
+        L.cosa_page_select.argtypes = [D, i32, vp, vp, PB, vp, vp, vp]
+        L.cosa_decode_workspace_bytes.restype = size
+        L.cosa_decode_workspace_bytes.argtypes = [D]
+        L.cosa_decode_attention.restype = S
+        L.cosa_decode_attention.argtypes = [D, vp, KV, vp, vp, size, vp, vp, vp]
+        L.cosa_decode_attention_listed.restype = S
+        L.cosa_decode_attention_listed.argtypes = [D, vp, KV, vp, vp, vp, i32, vp, size, vp, vp, vp]
+        L.cosa_decode_sparse_workspace_layout.restype = S
+        L.cosa_decode_sparse_workspace_layout.argtypes = [D, PB,
+                                                          ctypes.POINTER(CosaDecodeSparseLayout)]
+        L.cosa_decode_sparse_workspace_bytes.restype = size
+        L.cosa_decode_sparse_workspace_bytes.argtypes = [D, PB]
+        L.cosa_decode_sparse.restype = S
+        L.cosa_decode_sparse.argtypes = [D, vp, KV, vp, vp, PB, vp, size, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -416,3 +475,139 @@ def cosa_prefill_paged_varlen(problem, vl: CosaVarlen, q, kv: CosaPagedKv, sel: 
     _check(lib().cosa_prefill_paged_varlen(ctypes.byref(p), _vlref(vl), _ptr(q), _kvref(kv),
                                            ctypes.byref(sel), skp, _ptr(workspace),
                                            workspace_bytes, _ptr(o), _stream(stream)))
+
+
+# ---- decode-side operators (include/cosa_decode.h)
+
+def _decode_stream(stream, *tensors) -> Optional[int]:
+    """Stream of a call; None: the current stream of the device that holds the tensors, which must
+    be one device."""
+    devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
+    if len(devices) > 1:
+        raise ValueError("tensors must live on one device, not on "
+                         + " and ".join(sorted(map(str, devices))))
+    if stream is None:
+        import torch
+        return torch.cuda.current_stream(devices.pop() if devices else None).cuda_stream
+    if not isinstance(stream, int) and devices and stream.device != devices.copy().pop():
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {devices.pop()}")
+    return _stream(stream)
+
+
+def _rows(t, stride: int):
+    """Pointer and row stride (elements) of rows [n, heads, head_dim]: a tensor whose rows are dense
+    but may lie apart, or a raw pointer with the given stride."""
+    if t is None or isinstance(t, int):
+        return t, stride
+    if not t.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if t.dim() != 3 or (t.numel() and not t[0].is_contiguous()):
+        raise ValueError("rows must be [n, heads, head_dim] with dense heads and head_dim")
+    own = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    if own < t.shape[1] * t.shape[2]:
+        raise ValueError("rows must not overlap")
+    if stride and stride != own and t.shape[0] > 1:
+        raise ValueError(f"row stride {stride} given for a tensor with row stride {own}")
+    return t.data_ptr(), own
+
+
+def _dprob(problem, q=None):
+    """C problem and query pointer; the query tensor's own row stride goes into the problem."""
+    p = problem.c() if isinstance(problem, DecodeProblem) else problem
+    ptr, stride = _rows(q, p.q_stride)
+    if stride != p.q_stride:
+        p = CosaDecodeProblem(p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, p.max_pages, stride,
+                              p.sm_scale)
+    return p, ptr
+
+
+def page_budget(max_pages: int, min_pages: int = 1, fraction: float = 1.0, sink_pages: int = 1,
+                recent_pages: int = 1) -> CosaPageBudget:
+    """cosa_page_budget; by default up to max_pages pages of every sequence."""
+    return CosaPageBudget(fraction, min_pages, max_pages, sink_pages, recent_pages)
+
+
+def cosa_page_map(batch: int, page_size: int, max_pages: int, cached_lens, new_lens, free_pages,
+                  free_capacity: int, n_free, page_table, seq_lens, cu_new, slots, max_new: int,
+                  n_taken, stream=None):
+    s = _decode_stream(stream, cached_lens, new_lens, free_pages, n_free, page_table, seq_lens,
+                       cu_new, slots, n_taken)
+    _check(lib().cosa_page_map(batch, page_size, max_pages, _ptr(cached_lens), _ptr(new_lens),
+                               _ptr(free_pages), free_capacity, _ptr(n_free), _ptr(page_table),
+                               _ptr(seq_lens), _ptr(cu_new), _ptr(slots), max_new, _ptr(n_taken),
+                               s))
+
+
+def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, k_cache, v_cache,
+                   bounds, n_tokens: int, k, v, slots, k_stride: int = 0, v_stride: int = 0,
+                   stream=None):
+    """k and v: [n_tokens, n_kv_heads, head_dim] tensors, slices of a fused projection among them
+    (their row strides are taken from the tensors)."""
+    s = _decode_stream(stream, k_cache, v_cache, bounds, k, v, slots)
+    kp, k_stride = _rows(k, k_stride)
+    vp, v_stride = _rows(v, v_stride)
+    _check(lib().cosa_kv_append(n_kv_heads, head_dim, page_size, n_pages, _ptr(k_cache),
+                                _ptr(v_cache), _ptr(bounds), n_tokens, kp, k_stride, vp, v_stride,
+                                _ptr(slots), s))
+
+
+def cosa_page_score(problem, q, kv: CosaPagedKv, bounds, seq_lens, score, stream=None):
+    s = _decode_stream(stream, q, bounds, seq_lens, score)
+    p, qp = _dprob(problem, q)
+    _check(lib().cosa_page_score(ctypes.byref(p), qp, _kvref(kv), _ptr(bounds), _ptr(seq_lens),
+                                 _ptr(score), s))
+
+
+def cosa_page_select(problem, page_size: int, seq_lens, score, budget: CosaPageBudget, pages, count,
+                     stream=None):
+    s = _decode_stream(stream, seq_lens, score, pages, count)
+    p, _ = _dprob(problem)
+    _check(lib().cosa_page_select(ctypes.byref(p), page_size, _ptr(seq_lens), _ptr(score),
+                                  _kvref(budget), _ptr(pages), _ptr(count), s))
+
+
+def cosa_decode_workspace_bytes(problem) -> int:
+    p, _ = _dprob(problem)
+    n = int(lib().cosa_decode_workspace_bytes(ctypes.byref(p)))
+    if n == 0:
+        raise CosaError(COSA_ERR_INVALID_ARG, cosa_last_error())
+    return n
+
+
+def cosa_decode_attention(problem, q, kv: CosaPagedKv, seq_lens, workspace, workspace_bytes: int, o,
+                          lse=None, stream=None):
+    s = _decode_stream(stream, q, seq_lens, workspace, o, lse)
+    p, qp = _dprob(problem, q)
+    _check(lib().cosa_decode_attention(ctypes.byref(p), qp, _kvref(kv), _ptr(seq_lens),
+                                       _ptr(workspace), workspace_bytes, _ptr(o), _ptr(lse), s))
+
+
+def cosa_decode_attention_listed(problem, q, kv: CosaPagedKv, seq_lens, pages, count,
+                                 list_pages: int, workspace, workspace_bytes: int, o, lse=None,
+                                 stream=None):
+    s = _decode_stream(stream, q, seq_lens, pages, count, workspace, o, lse)
+    p, qp = _dprob(problem, q)
+    _check(lib().cosa_decode_attention_listed(ctypes.byref(p), qp, _kvref(kv), _ptr(seq_lens),
+                                              _ptr(pages), _ptr(count), list_pages, _ptr(workspace),
+                                              workspace_bytes, _ptr(o), _ptr(lse), s))
+
+
+def cosa_decode_sparse_workspace_layout(problem, budget: CosaPageBudget) -> CosaDecodeSparseLayout:
+    p, _ = _dprob(problem)
+    out = CosaDecodeSparseLayout()
+    _check(lib().cosa_decode_sparse_workspace_layout(ctypes.byref(p), _kvref(budget),
+                                                     ctypes.byref(out)))
+    return out
+
+
+def cosa_decode_sparse_workspace_bytes(problem, budget: CosaPageBudget) -> int:
+    return int(cosa_decode_sparse_workspace_layout(problem, budget).total)
+
+
+def cosa_decode_sparse(problem, q, kv: CosaPagedKv, bounds, seq_lens, budget: CosaPageBudget,
+                       workspace, workspace_bytes: int, o, lse=None, stream=None):
+    s = _decode_stream(stream, q, bounds, seq_lens, workspace, o, lse)
+    p, qp = _dprob(problem, q)
+    _check(lib().cosa_decode_sparse(ctypes.byref(p), qp, _kvref(kv), _ptr(bounds), _ptr(seq_lens),
+                                    _kvref(budget), _ptr(workspace), workspace_bytes, _ptr(o),
+                                    _ptr(lse), s))

@@ -19,7 +19,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libcosa.so")
-SOURCES = ["cosa_api.hip", "attention.hip", "kap_score.hip", "kap_select.hip", "block_mass.hip"]
+SOURCES = ["cosa_api.hip", "attention.hip", "kap_score.hip", "kap_select.hip", "block_mass.hip",
+           "decode_api.hip", "page_map.hip", "kv_append.hip", "page_score.hip", "page_select.hip",
+           "decode_attention.hip"]
 
 ARCH = "gfx950"
 COMMON = [

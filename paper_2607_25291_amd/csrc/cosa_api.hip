@@ -5,8 +5,8 @@
 #include <stdio.h>
 
 #include <mutex>
-#include <string>
 
+#include "api_status.h"
 #include "cosa.h"
 #include "cosa_internal.h"
 
@@ -17,28 +17,39 @@ static_assert(COSA_MAX_PACKED_SEQS == cosa::kMaxPackedSeqs, "packing limit of th
 // looked up once per device (scratch_of_device) and used everywhere the host needs the array.
 static __device__ __align__(256) unsigned char scratch[COSA_NOALLOC_SCRATCH_BYTES];
 
-namespace {
+namespace cosa {
 
-thread_local std::string g_last_error;
+namespace {
+thread_local char g_last_error[640] = "";
+}  // namespace
 
 cosa_status fail(cosa_status st, const char* fmt, ...) {
-  char buf[512];
+  const int n = snprintf(g_last_error, sizeof g_last_error, "%s: ", cosa_status_string(st));
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  vsnprintf(g_last_error + n, sizeof g_last_error - n, fmt, ap);
   va_end(ap);
-  g_last_error = std::string(cosa_status_string(st)) + ": " + buf;
   return st;
 }
 
 cosa_status ok() {
-  g_last_error.clear();
+  g_last_error[0] = '\0';
   return COSA_OK;
 }
 
 cosa_status hip_fail(hipError_t e, const char* what) {
   return fail(COSA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace cosa
+
+namespace {
+
+using cosa::align256;
+using cosa::as_stream;
+using cosa::fail;
+using cosa::hip_fail;
+using cosa::ok;
 
 // Validates the problem and fills the internal shape. `empty` is set for B == 0 or L == 0.
 cosa_status make_shape(const cosa_problem* p, cosa::Shape& sh, bool& empty) {
@@ -188,8 +199,6 @@ cosa_status check_varlen(const cosa_varlen* vl, const cosa::Shape& sh, const cos
   return ok();
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 cosa_workspace_layout layout_of(const cosa::Shape& sh) {
   const size_t rows = (size_t)sh.B * sh.Hkv * sh.nb;
   const size_t cells = rows * sh.nb;
@@ -203,8 +212,6 @@ cosa_workspace_layout layout_of(const cosa::Shape& sh) {
   l.total = align256(l.queue + cosa::kOskQueueBytes);
   return l;
 }
-
-hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
 // Device address of `scratch` on the GPU that runs `stream` (the current device for the null
 // stream), taken once per device with that device current and kept for later calls.
@@ -310,7 +317,7 @@ const char* cosa_status_string(cosa_status status) {
   return "COSA_ERR_UNKNOWN";
 }
 
-const char* cosa_last_error(void) { return g_last_error.c_str(); }
+const char* cosa_last_error(void) { return cosa::g_last_error; }
 
 cosa_status cosa_kap_score(const cosa_problem* problem, const void* q, const void* k, float* score,
                            uint8_t* hrm, void* stream) {

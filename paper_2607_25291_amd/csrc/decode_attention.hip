@@ -1,0 +1,411 @@
+// Attention of one new token per sequence over a paged KV cache, for gfx950: split over the tokens and
+// joined.
+//
+// A unit is (sequence, KV head, up to 16 query heads of its group). 32 keys at a time, a wave computes
+// S^T = K Q^T and O^T += V^T P^T with 16x16x32 MFMAs, the query heads as columns. K operands come straight
+// from the cache (lane: key l % 16, 16 bytes of its row). V operands too: lane (r, gq) reads the 16 bytes at
+// columns 8 r .. 8 r + 7 of eight keys, an 8 x 8 square that 32 byte permutes turn into eight operands
+// (operand e: rows d = 8 r + e, the lane's eight keys as k). Which keys those are is free as long as P has
+// the same order, so they are the keys whose logits the lane holds after K Q^T: P never leaves its lanes,
+// and nothing passes through LDS until a unit's end.
+//
+// The units' 128-token tiles form one sequence of work that a fixed grid cuts into equal ranges, whatever the lengths
+// are (the host does not know them): every workgroup scans the lengths and finds its range. A
+// unit that crosses ranges leaves one partial result (running maximum, sum, unnormalised O) in each, and
+// a second kernel joins them in order.
+//
+// Bound: HBM. A token costs 512 bytes per KV head and 4 G d flops, G flops per byte.
+#include "cosa_device.h"
+#include "decode_internal.h"
+#include "select_wave.h"
+
+namespace cosa {
+namespace {
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kTile = 128;     // tokens of a tile: 32 per wave
+constexpr int kGrid = 512;     // workgroups that share the tiles: two per CU
+constexpr int kWholeTiles = 4; // units of at most this many tiles are not split
+constexpr int kRows = 16;      // query heads of a unit
+constexpr int kPartStride = kRows * (kHeadDim + 2);  // floats of a partial result
+
+struct DecodeParams {
+  const uint16_t *q, *kc, *vc;
+  const int32_t *table, *seq_lens, *pages, *count;
+  float* part;    // [2 * grid][kPartStride]: the partial results of a workgroup's first and last unit
+  int2* rec;      // [grid]: the unit that starts in a workgroup and goes on behind it, and the last workgroup it reaches
+  uint16_t* o;
+  float* lse;
+  int Hq, Hkv, G, QG;
+  int max_pages, log2_page, list_pages;
+  int items, mult;  // items of equal tile counts in a row: sequences (mult Hkv * QG) or KV heads (mult QG)
+  long long q_stride, n_pages;
+  float scale_log2;
+};
+
+__device__ __forceinline__ f32x4_t mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float xmax16(float v) { return fmaxf(v, __shfl_xor(v, 16, 64)); }
+
+__device__ __forceinline__ int seq_len(const DecodeParams& P, int n) {
+  return min(max(P.seq_lens[n], 0), P.max_pages << P.log2_page);
+}
+
+// Tokens an item walks: the sequence, or its list (pages in full).
+template <bool LISTED>
+__device__ __forceinline__ int item_tokens(const DecodeParams& P, int i) {
+  if (LISTED) return min(max(P.count[i], 0), P.list_pages) << P.log2_page;
+  return seq_len(P, i);
+}
+__device__ __forceinline__ int tiles_of(int tokens) {
+  return max((int)(((unsigned)tokens + kTile - 1) / kTile), 1);
+}
+
+// Two fp32 values as bf16 pairs: the nearest ones, and what they leave.
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint32_t& lo) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t h = __builtin_convertvector((f32x2_t{a, b}), bf16x2_t);
+  hi = __builtin_bit_cast(uint32_t, h);
+  const float ra = a - __uint_as_float(hi << 16), rb = b - __uint_as_float(hi & 0xffff0000u);
+  lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{ra, rb}), bf16x2_t));
+}
+
+struct Tile {
+  u32x4_t k[2][4], v[8];
+};
+
+// One unit's tiles [t0, t1) by the workgroup; the result goes to o and lse (part == nullptr) or to part.
+template <bool LISTED>
+__device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg, int tokens, int t0, int t1, float* part,
+                     float (*so)[kRows][kHeadDim + 4], float (*sm)[kRows], float (*sl)[kRows]) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gq = lane >> 4;
+  const int rows = min(P.G - qg * kRows, kRows);
+  const int h0 = g * P.G + qg * kRows;
+  const int page = 1 << P.log2_page;
+  const int len = seq_len(P, n);
+
+  u32x4_t qf[4];
+  const uint16_t* q = P.q + (size_t)n * P.q_stride + (size_t)(h0 + min(r, rows - 1)) * kHeadDim + gq * 8;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) qf[c] = ldg16(q + c * 32);
+
+  f32x4_t acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;  // running maximum (log2 units) of column r, and this lane's share of its sum
+
+  const unsigned begin = (unsigned)t0 * kTile + w * 32;
+  const unsigned end = min((unsigned)t1 * kTile, (unsigned)tokens);
+  const int steps = begin < end ? (int)((end - begin + kTile - 1) / kTile) : 0;
+  const int32_t* row = P.table + (size_t)n * P.max_pages;
+  const int32_t* list = LISTED ? P.pages + (size_t)(n * P.Hkv + g) * P.list_pages : nullptr;
+
+  // Pages of steps i0 .. i0 + 63, one per lane: physical page and valid keys of either half.
+  int pg[2], valid[2];
+  const auto look_up = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const unsigned pos = begin + (unsigned)(i0 + lane) * kTile + h * 16;
+      pg[h] = 0;
+      valid[h] = 0;
+      if (i0 + lane < steps && pos < end) {
+        int j = (int)(pos >> P.log2_page);
+        if (LISTED) j = list[j];
+        const bool in = j >= 0 && j < P.max_pages;
+        const int64_t left = in ? (int64_t)len - (((int64_t)j << P.log2_page) + (pos & (unsigned)(page - 1))) : 0;
+        valid[h] = (int)min(max(left, (int64_t)0), (int64_t)16);
+        if (valid[h] > 0) {
+          const int p = row[j];
+          pg[h] = p >= 0 && p < P.n_pages ? p : 0;
+        }
+      }
+    }
+  };
+  const auto load = [&](Tile& T, int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const unsigned pos = begin + (unsigned)i * kTile + h * 16;
+      const size_t p = (size_t)(unsigned)__builtin_amdgcn_readlane(pg[h], i & 63);
+      const size_t at = (((p * P.Hkv + g) << P.log2_page) + (pos & (unsigned)(page - 1))) * kHeadDim;
+      const uint16_t* kp = P.kc + at;
+      const uint16_t* vp = P.vc + at;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) T.k[h][c] = ldg16(kp + (r * kHeadDim + c * 32 + gq * 8));
+#pragma unroll
+      for (int c = 0; c < 4; ++c) T.v[h * 4 + c] = ldg16(vp + ((gq * 4 + c) * kHeadDim + r * 8));
+    }
+  };
+  const auto compute = [&](Tile& T, int v0, int v1) __attribute__((always_inline)) {
+    f32x4_t s[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[h] = mfma16(T.k[h][c], qf[c], s[h]);
+    }
+    if (v0 < 16 || v1 < 16) {  // keys behind the sequence: no weight, and values that cannot spoil the sum
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (gq * 4 + i >= (h ? v1 : v0)) {
+            s[h][i] = -INFINITY;
+            T.v[h * 4 + i] = u32x4_t{0, 0, 0, 0};
+          }
+    }
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    mx = half_max(xmax16(mx)) * P.scale_log2;
+    const float mn = fmaxf(m, mx);
+    const float base = mn == -INFINITY ? 0.f : mn;
+    const float alpha = __builtin_amdgcn_exp2f(m - base);
+    float p[8], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], P.scale_log2, -base));
+      sum += p[i];
+    }
+    l = l * alpha + sum;
+    m = mn;
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[e][i] *= alpha;
+    }
+    u32x4_t ph, pl;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t a, b;
+      split_bf16(p[2 * i], p[2 * i + 1], a, b);
+      ph[i] = a;
+      pl[i] = b;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      // operand e: element e of the lane's eight keys
+      u32x4_t a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        a[i] = __builtin_amdgcn_perm(T.v[2 * i + 1][e >> 1], T.v[2 * i][e >> 1],
+                                     (e & 1) ? 0x07060302u : 0x05040100u);
+      acc[e] = mfma16(a, ph, acc[e]);
+      acc[e] = mfma16(a, pl, acc[e]);
+    }
+  };
+
+  if (steps > 0) {
+    Tile A, B;
+    look_up(0);
+    load(A, 0);
+    for (int i = 0; i < steps; i += 2) {
+      int v0 = __builtin_amdgcn_readlane(valid[0], i & 63), v1 = __builtin_amdgcn_readlane(valid[1], i & 63);
+      if (i + 1 < steps) load(B, i + 1);
+      const int b0 = __builtin_amdgcn_readlane(valid[0], (i + 1) & 63);
+      const int b1 = __builtin_amdgcn_readlane(valid[1], (i + 1) & 63);
+      if (((i + 2) & 63) == 0) look_up(i + 2);
+      compute(A, v0, v1);
+      if (i + 2 < steps) load(A, i + 2);
+      if (i + 1 < steps) compute(B, b0, b1);
+    }
+  }
+
+  // The four waves' results: lane (r, gq) holds columns d = 8 (4 gq + i) + e of query head r.
+  l += __shfl_xor(l, 16, 64);
+  l = half_sum(l);
+  if (r < rows) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* to = &so[w][r][8 * (4 * gq + i)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) to[e] = acc[e][i];
+    }
+    if (gq == 0) {
+      sm[w][r] = m;
+      sl[w][r] = l;
+    }
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < rows * kHeadDim; x += kThreads) {
+    const int hh = x >> 7, d = x & 127;
+    float M = sm[0][hh];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) M = fmaxf(M, sm[i][hh]);
+    const float base = M == -INFINITY ? 0.f : M;
+    float L = 0.f, O = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float a = __builtin_amdgcn_exp2f(sm[i][hh] - base);
+      L += a * sl[i][hh];
+      O += a * so[i][hh][d];
+    }
+    if (part) {
+      part[hh * kHeadDim + d] = O;
+      if (d == 0) {
+        part[kRows * kHeadDim + hh] = M;
+        part[kRows * (kHeadDim + 1) + hh] = L;
+      }
+    } else {
+      const size_t out = (size_t)n * P.Hq + h0 + hh;
+      const __bf16 v = (__bf16)(M == -INFINITY ? 0.f : O / L);
+      P.o[out * kHeadDim + d] = __builtin_bit_cast(uint16_t, v);
+      if (P.lse && d == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
+    }
+  }
+  __syncthreads();  // so, sm and sl are used again
+}
+
+// WHOLE: a workgroup per unit, no splitting.
+template <bool LISTED, bool WHOLE>
+__global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
+  __shared__ float so[kWaves][kRows][kHeadDim + 4], sm[kWaves][kRows], sl[kWaves][kRows];
+  const auto unit = [&](int item, int sub, int t0, int t1, int tokens, float* part) __attribute__((always_inline)) {
+    const int n = LISTED ? item / P.Hkv : item;
+    const int g = LISTED ? item % P.Hkv : sub / P.QG;
+    walk<LISTED>(P, n, g, sub % P.QG, tokens, t0, t1, part, so, sm, sl);
+  };
+  if (WHOLE) {
+    const int item = blockIdx.x / P.mult;
+    const int tokens = item_tokens<LISTED>(P, item);
+    unit(item, blockIdx.x % P.mult, 0, tiles_of(tokens), tokens, nullptr);
+    return;
+  }
+  __shared__ uint32_t waves[kWaves];
+  __shared__ int found[2];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  // Tiles of the items before each thread's share of them, and all tiles.
+  const int per = (P.items + kThreads - 1) / kThreads;
+  const int i0 = min((int)threadIdx.x * per, P.items), i1 = min(i0 + per, P.items);
+  uint32_t sum = 0;
+  for (int i = i0; i < i1; ++i) sum += (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+  const uint32_t incl = wave_incl_scan(sum, lane);
+  if (lane == 63) waves[w] = incl;
+  __syncthreads();
+  uint32_t at = incl - sum, total = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    if (i < w) at += waves[i];
+    total += waves[i];
+  }
+  const uint64_t W = (uint64_t)total * P.mult;
+  const uint64_t N = W < gridDim.x ? W : gridDim.x;
+  if (threadIdx.x == 0) P.rec[blockIdx.x] = int2{-1, 0};
+  if (blockIdx.x >= N) return;
+  uint64_t a = blockIdx.x * W / N;
+  const uint64_t b = (blockIdx.x + 1) * W / N;
+  const uint32_t x = (uint32_t)(a / P.mult);
+  if (x >= at && x < at + sum) {
+    int i = i0;
+    for (;; ++i) {
+      const uint32_t t = (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+      if (x < at + t) break;
+      at += t;
+    }
+    found[0] = i;
+    found[1] = (int)at;
+  }
+  __syncthreads();
+  int item = __builtin_amdgcn_readfirstlane(found[0]);
+  int tokens = item_tokens<LISTED>(P, item);
+  int tiles = tiles_of(tokens);
+  const uint32_t rem = (uint32_t)(a - (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(found[1]) * P.mult);
+  int sub = (int)(rem / (uint32_t)tiles), t0 = (int)(rem % (uint32_t)tiles);
+  for (;;) {
+    const int t1 = (int)(b - a < (uint64_t)(tiles - t0) ? t0 + (b - a) : tiles);
+    float* part = nullptr;
+    if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride;
+    if (t0 == 0 && t1 < tiles && threadIdx.x == 0) {
+      const uint64_t end = a + tiles;  // behind the unit's last tile
+      P.rec[blockIdx.x] = int2{item * P.mult + sub, (int)((end * N - 1) / W)};
+    }
+    unit(item, sub, t0, t1, tokens, part);
+    a += t1 - t0;
+    if (a >= b) return;
+    t0 = 0;
+    if (++sub == P.mult) {
+      sub = 0;
+      tokens = item_tokens<LISTED>(P, ++item);
+      tiles = tiles_of(tokens);
+    }
+  }
+}
+
+// Joins the partial results of the unit that starts in workgroup blockIdx.x and goes on behind it, query head
+// blockIdx.y of the unit.
+template <bool LISTED>
+__global__ __launch_bounds__(kHeadDim) void join_kernel(DecodeParams P) {
+  __shared__ float red[2];
+  const int2 rec = P.rec[blockIdx.x];
+  if (rec.x < 0) return;
+  const int item = rec.x / P.mult, sub = rec.x % P.mult;
+  const int n = LISTED ? item / P.Hkv : item, g = LISTED ? item % P.Hkv : sub / P.QG, qg = sub % P.QG;
+  const int hh = blockIdx.y, d = threadIdx.x;
+  if (qg * kRows + hh >= P.G) return;
+  const int first = blockIdx.x, n_parts = rec.y - first + 1;
+  const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * kPartStride; };
+  float M = -INFINITY;
+  for (int i = d; i < n_parts; i += kHeadDim) M = fmaxf(M, part(i)[kRows * kHeadDim + hh]);
+  M = wave_max(M);
+  if ((d & 63) == 0) red[d >> 6] = M;
+  __syncthreads();
+  M = fmaxf(red[0], red[1]);
+  const float base = M == -INFINITY ? 0.f : M;
+  float L = 0.f, O = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < n_parts; ++i) {
+    const float* p = part(i);
+    const float a = __builtin_amdgcn_exp2f(p[kRows * kHeadDim + hh] - base);
+    L += a * p[kRows * (kHeadDim + 1) + hh];
+    O += a * p[hh * kHeadDim + d];
+  }
+  const size_t out = (size_t)n * P.Hq + (size_t)g * P.G + qg * kRows + hh;
+  const __bf16 v = (__bf16)(M == -INFINITY ? 0.f : O / L);
+  P.o[out * kHeadDim + d] = __builtin_bit_cast(uint16_t, v);
+  if (P.lse && d == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
+}
+
+template <bool LISTED>
+hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream) {
+  const long long units = (long long)P.items * P.mult, tiles = (tokens + kTile - 1) / kTile;
+  if (tiles <= kWholeTiles) {
+    hipLaunchKernelGGL((decode_kernel<LISTED, true>), dim3((unsigned)units), dim3(kThreads), 0, stream, P);
+    return hipGetLastError();
+  }
+  const int grid = (int)std::min<long long>(units * tiles, kGrid);
+  hipLaunchKernelGGL((decode_kernel<LISTED, false>), dim3(grid), dim3(kThreads), 0, stream, P);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((join_kernel<LISTED>), dim3(grid, std::min(P.G, kRows)), dim3(kHeadDim), 0, stream, P);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t decode_workspace_bytes(const DecodeShape&) {
+  return ((size_t)kGrid * sizeof(int2) + 255) / 256 * 256 + (size_t)kGrid * 2 * kPartStride * sizeof(float);
+}
+
+bool decode_fits(const DecodeShape& sh, long long tokens) {
+  const long long QG = (sh.G + kRows - 1) / kRows, tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1);
+  return (long long)sh.B * sh.Hkv * QG < (1ll << 24) && (long long)sh.B * sh.Hkv * QG * tiles < (1ll << 31);
+}
+
+hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream) {
+  const int QG = (sh.G + kRows - 1) / kRows;
+  int2* rec = static_cast<int2*>(a.workspace);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + ((size_t)kGrid * sizeof(int2) + 255) / 256 * 256);
+  const bool listed = a.pages != nullptr;
+  const DecodeParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.pages, a.count, part, rec, a.o, a.lse,
+                       sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages, sh.log2_page, a.list_pages,
+                       listed ? sh.B * sh.Hkv : sh.B, listed ? QG : sh.Hkv * QG, sh.q_stride, sh.n_pages,
+                       sh.scale * 1.4426950408889634f};
+  return listed ? launch_t<true>(P, (long long)a.list_pages << sh.log2_page, stream)
+                : launch_t<false>(P, sh.cap(), stream);
+}
+
+}  // namespace cosa
