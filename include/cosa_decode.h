@@ -37,7 +37,7 @@ extern "C" {
 
 /* One new token for each sequence of a batch. The paged cache is a cosa_paged_kv, with page_table
  * [batch, max_pages]: entry [n, j] is the physical page of tokens j * page_size .. of sequence n. Entries
- * behind a sequence's last page are not read; an entry outside [0, n_pages) is read as page 0. */
+ * behind a sequence's last page are not used; an entry outside [0, n_pages) is read as page 0. */
 typedef struct {
   int32_t batch;      /* B >= 0                                                                   */
   int32_t n_q_heads;  /* Hq, a multiple of n_kv_heads; query head h reads KV head h / (Hq / Hkv)   */
