@@ -2,9 +2,9 @@
 // head).
 //
 // The rows' maxima, then one 32-bit key per page in LDS whose order is the order of selection (forced
-// pages, NaN, then descending s). A radix selection over four 8-bit digits finds the K-th largest key and
-// how many pages that equal it are kept; a scan over the pages then packs the kept ones in ascending
-// order, so the list needs no sort.
+// pages, NaN, then descending s). A radix selection finds the K-th largest key and how many pages that
+// equal it are kept; a scan over the pages then packs the kept ones in ascending order, so the list needs
+// no sort.
 #include <mutex>
 
 #include "cosa_device.h"
@@ -14,8 +14,6 @@
 namespace cosa {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr uint32_t kForced = 0xffffffffu, kNan = 0xfffffffeu;
 
 __device__ __forceinline__ uint32_t key_of(float s) {
@@ -24,11 +22,23 @@ __device__ __forceinline__ uint32_t key_of(float s) {
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-__global__ __launch_bounds__(kThreads) void page_select_kernel(PageSelectArgs A) {
+// Scores of one head at pages j, j + T, j + 2 T, j + 3 T (-inf behind the row).
+template <int T>
+__device__ __forceinline__ void load4(float (&x)[4], const float* row, int j, int np) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = j + i * T < np ? row[j + i * T] : -INFINITY;
+}
+
+constexpr int kBins = 2048;
+
+template <int T>
+__global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
+  constexpr int kWaves = T / 64, kPer = kBins / T;
   extern __shared__ uint32_t lds[];
-  float* top = reinterpret_cast<float*>(lds);  // row maxima of the group's heads
-  uint32_t* keys = lds + A.G;
-  __shared__ uint32_t hist[256], waves[kWaves], pick[2];
+  uint32_t* keys = lds;                                                       // max_pages, in fours
+  float* top = reinterpret_cast<float*>(lds + (A.max_pages + 3) / 4 * 4);     // row maxima of the group's heads
+  __shared__ uint32_t hist[kBins], waves[kWaves], pick[3];
+  __shared__ float part[4][kWaves];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int u = blockIdx.x, n = u / A.Hkv, g = u % A.Hkv;
   const int page = 1 << A.log2_page;
@@ -38,102 +48,155 @@ __global__ __launch_bounds__(kThreads) void page_select_kernel(PageSelectArgs A)
   const int frac = (int)((A.fraction_micro * np + 999999) / 1000000);
   const int K = min(np, max(A.sink + A.recent, min(A.max_keep, max(A.min_keep, frac))));
   if (threadIdx.x == 0) A.count[u] = K;
-  for (int j = K + threadIdx.x; j < A.max_keep; j += kThreads) out[j] = -1;
+  for (int j = K + threadIdx.x; j < A.max_keep; j += T) out[j] = -1;
   if (K == np) {
-    for (int j = threadIdx.x; j < K; j += kThreads) out[j] = j;
+    for (int j = threadIdx.x; j < K; j += T) out[j] = j;
     return;
   }
   const float* score = A.score + ((size_t)n * A.Hq + (size_t)g * A.G) * A.max_pages;
-  for (int h = w; h < A.G; h += kWaves) {
-    float m = -INFINITY;
-    for (int j = lane; j < np; j += 64) m = fmaxf(m, score[(size_t)h * A.max_pages + j]);
-    m = wave_max(m);
-    if (lane == 0) top[h] = m;
+  // Row maxima, four heads at a time.
+  for (int h0 = 0; h0 < A.G; h0 += 4) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    for (int j = threadIdx.x; j < np; j += 4 * T) {
+      float x[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) load4<T>(x[k], score + (size_t)min(h0 + k, A.G - 1) * A.max_pages, j, np);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], fmaxf(fmaxf(x[k][0], x[k][1]), fmaxf(x[k][2], x[k][3])));
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = wave_max(m[k]);
+      if (lane == 0) part[k][w] = m[k];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4 && h0 + (int)threadIdx.x < A.G) {
+      float t = part[threadIdx.x][0];
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) t = fmaxf(t, part[threadIdx.x][i]);
+      top[h0 + threadIdx.x] = t;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int j = threadIdx.x; j < np; j += kThreads) {
-    float s = -INFINITY;
-    for (int h = 0; h < A.G; ++h) s = vmax(s, score[(size_t)h * A.max_pages + j] - top[h]);
-    keys[j] = j < A.sink || j >= np - A.recent ? kForced : key_of(s);
+  for (int j = threadIdx.x; j < np; j += 4 * T) {
+    float s[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 4
+    for (int h = 0; h < A.G; ++h) {
+      float x[4];
+      load4<T>(x, score + (size_t)h * A.max_pages, j, np);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = vmax(s[i], x[i] - top[h]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int jj = j + i * T;
+      if (jj < np) keys[jj] = jj < A.sink || jj >= np - A.recent ? kForced : key_of(s[i]);
+    }
   }
 
+  // The K-th largest key by its digits of 11, 11 and 10 bits; it ends early where a digit's pages are all kept.
   uint32_t prefix = 0, mask = 0, want = (uint32_t)K;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[threadIdx.x] = 0;
-    __syncthreads();
-    for (int j = threadIdx.x; j < np; j += kThreads)
-      if ((keys[j] & mask) == prefix) atomicAdd(&hist[(keys[j] >> shift) & 255u], 1u);
-    __syncthreads();
-    if (w == 0) {
-      // lane l holds bins 255 - 4 l .. 252 - 4 l: from the largest digit down
-      uint32_t c[4], s = 0;
+  bool whole = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s += c[i] = hist[255 - 4 * lane - i];
-      const uint32_t incl = wave_incl_scan(s, lane);
-      uint32_t before = incl - s;
-      if (before < want && incl >= want) {
+  for (int pass = 0; pass < 3 && !whole; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t digits = pass == 2 ? 1023u : 2047u;
+    for (int i = threadIdx.x; i < kBins; i += T) hist[i] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < np; j += T) {
+      const uint32_t k = keys[j];
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
+    }
+    __syncthreads();
+    // Thread t counts bins from the largest digit down: kBins - 1 - t kPer, ...
+    uint32_t c[kPer], s = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < want && before + c[i] >= want) {
-            pick[0] = 255u - 4u * lane - i;
-            pick[1] = want - before;
-          }
-          before += c[i];
+    for (int i = 0; i < kPer; ++i) s += c[i] = hist[kBins - 1 - (int)threadIdx.x * kPer - i];
+    const uint32_t incl = wave_incl_scan(s, lane);
+    if (lane == 63) waves[w] = incl;
+    __syncthreads();
+    uint32_t before = incl - s;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i)
+      if (i < w) before += waves[i];
+    if (before < want && before + s >= want) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (before < want && before + c[i] >= want) {
+          pick[0] = (uint32_t)(kBins - 1 - (int)threadIdx.x * kPer - i);
+          pick[1] = want - before;
+          pick[2] = c[i];
         }
+        before += c[i];
       }
     }
     __syncthreads();
     prefix |= pick[0] << shift;
-    mask |= 255u << shift;
+    mask |= digits << shift;
     want = pick[1];
+    whole = want == pick[2];
   }
 
-  // prefix is the K-th largest key; the first `want` pages that equal it are kept.
+  // Kept: keys above the prefix, and of those that share it all (whole) or the first `want` pages.
   uint32_t kept = 0, ties = 0;  // of the pages before
-  for (int j0 = 0; j0 < np; j0 += kThreads) {
-    const int j = j0 + threadIdx.x;
-    const uint32_t key = j < np ? keys[j] : 0u;
-    const bool above = j < np && key > prefix, tie = j < np && key == prefix;
-    const uint64_t ba = __ballot(above), bt = __ballot(tie);
+  for (int j0 = 0; j0 < np; j0 += 4 * T) {
+    const int j = j0 + (int)threadIdx.x * 4;
+    uint32_t mine = 0;
+    uint32_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      k[i] = j + i < np ? keys[j + i] & mask : 0u;
+      if (j + i < np) mine += k[i] > prefix ? 0x10000u : k[i] == prefix ? 1u : 0u;
+    }
+    const uint32_t incl = wave_incl_scan(mine, lane);
     __syncthreads();
-    if (lane == 0) waves[w] = ((uint32_t)__popcll(ba) << 16) | (uint32_t)__popcll(bt);
+    if (lane == 63) waves[w] = incl;
     __syncthreads();
-    uint32_t a = kept, t = ties;
+    uint32_t before = incl - mine, all = 0;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      if (i < w) {
-        a += waves[i] >> 16;
-        t += waves[i] & 0xffffu;
-      }
-      kept += waves[i] >> 16;
-      ties += waves[i] & 0xffffu;
+      if (i < w) before += waves[i];
+      all += waves[i];
     }
-    a += lanes_below(ba);
-    t += lanes_below(bt);
-    if (above || (tie && t < want)) out[a + min(t, want)] = j;
+    uint32_t a = kept + (before >> 16), t = ties + (before & 0xffffu);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (j + i >= np) break;
+      const bool above = k[i] > prefix, tie = k[i] == prefix;
+      if (above || (tie && t < want)) out[a + min(t, want)] = j + i;
+      a += above;
+      t += tie;
+    }
+    kept += all >> 16;
+    ties += all & 0xffffu;
   }
+}
+
+template <int T>
+hipError_t launch_t(const PageSelectArgs& a, hipStream_t stream) {
+  static std::mutex mu;
+  static bool granted[64] = {};
+  const size_t lds = ((size_t)(a.max_pages + 3) / 4 * 4 + a.G) * 4;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (lds > 48 * 1024) {
+    std::lock_guard<std::mutex> lock(mu);
+    if (dev < 0 || dev >= 64 || !granted[dev]) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(&page_select_kernel<T>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, (kMaxSelectPages + 4096) * 4);
+      if (e != hipSuccess) return e;
+      if (dev >= 0 && dev < 64) granted[dev] = true;
+    }
+  }
+  hipLaunchKernelGGL((page_select_kernel<T>), dim3(a.B * a.Hkv), dim3(T), lds, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_page_select(const PageSelectArgs& a, hipStream_t stream) {
-  static std::mutex mu;
-  static bool granted[64] = {};
-  const size_t lds = ((size_t)a.G + a.max_pages) * 4;
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  if (lds > 60 * 1024) {
-    std::lock_guard<std::mutex> lock(mu);
-    if (dev < 0 || dev >= 64 || !granted[dev]) {
-      e = hipFuncSetAttribute(reinterpret_cast<const void*>(&page_select_kernel),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024);
-      if (e != hipSuccess) return e;
-      if (dev >= 0 && dev < 64) granted[dev] = true;
-    }
-  }
-  hipLaunchKernelGGL(page_select_kernel, dim3(a.B * a.Hkv), dim3(kThreads), lds, stream, a);
-  return hipGetLastError();
+  return a.max_pages <= 1024 ? launch_t<256>(a, stream) : launch_t<1024>(a, stream);
 }
 
 }  // namespace cosa
