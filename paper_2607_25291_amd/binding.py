@@ -10,6 +10,7 @@ import ctypes
 import os
 import re
 from dataclasses import dataclass
+from functools import cached_property
 from typing import Optional
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -116,6 +117,7 @@ class DecodeProblem:
     q_stride: int = 0
     sm_scale: float = 0.0
 
+    @cached_property
     def c(self) -> CosaDecodeProblem:
         return CosaDecodeProblem(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
                                  self.max_pages, self.q_stride, self.sm_scale)
@@ -479,46 +481,70 @@ def cosa_prefill_paged_varlen(problem, vl: CosaVarlen, q, kv: CosaPagedKv, sel: 
 
 # ---- decode-side operators (include/cosa_decode.h)
 
-def _decode_stream(stream, *tensors) -> Optional[int]:
-    """Stream of a call; None: the current stream of the device that holds the tensors, which must
-    be one device."""
-    devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
-    if len(devices) > 1:
-        raise ValueError("tensors must live on one device, not on "
-                         + " and ".join(sorted(map(str, devices))))
+def _place(stream, *tensors):
+    """Stream of a call (None: the current one of the device that holds the tensors) and the tensors' device
+    pointers. They must be contiguous and share one device; None and raw pointers pass through."""
+    device, out = None, []
+    for t in tensors:
+        if t is not None and not isinstance(t, int):
+            device = _device(t, device)
+            if not t.is_contiguous():
+                raise ValueError("tensors must be contiguous")
+            t = t.data_ptr()
+        out.append(t)
+    return _stream_of(stream, device), out
+
+
+def _device(t, device: Optional[int]) -> int:
+    d = t.get_device()
+    if d != device:
+        if d < 0:
+            raise ValueError("tensors must live on the GPU")
+        if device is not None:
+            raise ValueError(f"tensors must live on one device, not on cuda:{device} and cuda:{d}")
+    return d
+
+
+def _stream_of(stream, device: Optional[int]) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream(devices.pop() if devices else None).cuda_stream
-    if not isinstance(stream, int) and devices and stream.device != devices.copy().pop():
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {devices.pop()}")
-    return _stream(stream)
+        return torch.cuda.current_stream(device).cuda_stream
+    if isinstance(stream, int):
+        return stream
+    if device is not None and stream.device.index != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{device}")
+    return stream.cuda_stream
 
 
-def _rows(t, stride: int):
+def _rows(t, stride: int, like=None):
     """Pointer and row stride (elements) of rows [n, heads, head_dim]: a tensor whose rows are dense
-    but may lie apart, or a raw pointer with the given stride."""
+    but may lie apart, on the device of the tensor `like`, or a raw pointer with the given stride."""
     if t is None or isinstance(t, int):
         return t, stride
-    if not t.is_cuda:
-        raise ValueError("tensors must live on the GPU")
-    if t.dim() != 3 or (t.numel() and not t[0].is_contiguous()):
-        raise ValueError("rows must be [n, heads, head_dim] with dense heads and head_dim")
-    own = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-    if own < t.shape[1] * t.shape[2]:
+    _device(t, None if like is None or isinstance(like, int) else like.get_device())
+    if t.dim() != 3:
+        raise ValueError("rows must be [n, heads, head_dim]")
+    n, heads, dim = t.shape
+    row, head, elem = t.stride()
+    if (elem != 1 and dim > 1) or (head != dim and heads > 1):
+        raise ValueError("rows must be dense in heads and head_dim")
+    if n <= 1:
+        row = heads * dim
+    if row < heads * dim:
         raise ValueError("rows must not overlap")
-    if stride and stride != own and t.shape[0] > 1:
-        raise ValueError(f"row stride {stride} given for a tensor with row stride {own}")
-    return t.data_ptr(), own
+    if stride and stride != row and n > 1:
+        raise ValueError(f"row stride {stride} given for a tensor with row stride {row}")
+    return t.data_ptr(), row
 
 
-def _dprob(problem, q=None):
+def _dprob(problem, q=None, like=None):
     """C problem and query pointer; the query tensor's own row stride goes into the problem."""
-    p = problem.c() if isinstance(problem, DecodeProblem) else problem
-    ptr, stride = _rows(q, p.q_stride)
-    if stride != p.q_stride:
+    p = problem.c if isinstance(problem, DecodeProblem) else problem
+    ptr, stride = _rows(q, p.q_stride, like)
+    if stride != p.q_stride and stride != p.n_q_heads * p.head_dim:
         p = CosaDecodeProblem(p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, p.max_pages, stride,
                               p.sm_scale)
-    return p, ptr
+    return ctypes.byref(p), ptr
 
 
 def page_budget(max_pages: int, min_pages: int = 1, fraction: float = 1.0, sink_pages: int = 1,
@@ -530,12 +556,10 @@ def page_budget(max_pages: int, min_pages: int = 1, fraction: float = 1.0, sink_
 def cosa_page_map(batch: int, page_size: int, max_pages: int, cached_lens, new_lens, free_pages,
                   free_capacity: int, n_free, page_table, seq_lens, cu_new, slots, max_new: int,
                   n_taken, stream=None):
-    s = _decode_stream(stream, cached_lens, new_lens, free_pages, n_free, page_table, seq_lens,
-                       cu_new, slots, n_taken)
-    _check(lib().cosa_page_map(batch, page_size, max_pages, _ptr(cached_lens), _ptr(new_lens),
-                               _ptr(free_pages), free_capacity, _ptr(n_free), _ptr(page_table),
-                               _ptr(seq_lens), _ptr(cu_new), _ptr(slots), max_new, _ptr(n_taken),
-                               s))
+    s, (cached, new, free, nf, table, lens, cu, sl, taken) = _place(
+        stream, cached_lens, new_lens, free_pages, n_free, page_table, seq_lens, cu_new, slots, n_taken)
+    _check(lib().cosa_page_map(batch, page_size, max_pages, cached, new, free, free_capacity, nf, table,
+                               lens, cu, sl, max_new, taken, s))
 
 
 def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, k_cache, v_cache,
@@ -543,32 +567,29 @@ def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
                    stream=None):
     """k and v: [n_tokens, n_kv_heads, head_dim] tensors, slices of a fused projection among them
     (their row strides are taken from the tensors)."""
-    s = _decode_stream(stream, k_cache, v_cache, bounds, k, v, slots)
-    kp, k_stride = _rows(k, k_stride)
-    vp, v_stride = _rows(v, v_stride)
-    _check(lib().cosa_kv_append(n_kv_heads, head_dim, page_size, n_pages, _ptr(k_cache),
-                                _ptr(v_cache), _ptr(bounds), n_tokens, kp, k_stride, vp, v_stride,
-                                _ptr(slots), s))
+    s, (kc, vc, b, sl) = _place(stream, k_cache, v_cache, bounds, slots)
+    kp, k_stride = _rows(k, k_stride, k_cache)
+    vp, v_stride = _rows(v, v_stride, k_cache)
+    _check(lib().cosa_kv_append(n_kv_heads, head_dim, page_size, n_pages, kc, vc, b, n_tokens, kp,
+                                k_stride, vp, v_stride, sl, s))
 
 
 def cosa_page_score(problem, q, kv: CosaPagedKv, bounds, seq_lens, score, stream=None):
-    s = _decode_stream(stream, q, bounds, seq_lens, score)
-    p, qp = _dprob(problem, q)
-    _check(lib().cosa_page_score(ctypes.byref(p), qp, _kvref(kv), _ptr(bounds), _ptr(seq_lens),
-                                 _ptr(score), s))
+    s, (b, lens, out) = _place(stream, bounds, seq_lens, score)
+    p, qp = _dprob(problem, q, score)
+    _check(lib().cosa_page_score(p, qp, _kvref(kv), b, lens, out, s))
 
 
 def cosa_page_select(problem, page_size: int, seq_lens, score, budget: CosaPageBudget, pages, count,
                      stream=None):
-    s = _decode_stream(stream, seq_lens, score, pages, count)
+    s, (lens, sc, pg, cnt) = _place(stream, seq_lens, score, pages, count)
     p, _ = _dprob(problem)
-    _check(lib().cosa_page_select(ctypes.byref(p), page_size, _ptr(seq_lens), _ptr(score),
-                                  _kvref(budget), _ptr(pages), _ptr(count), s))
+    _check(lib().cosa_page_select(p, page_size, lens, sc, _kvref(budget), pg, cnt, s))
 
 
 def cosa_decode_workspace_bytes(problem) -> int:
     p, _ = _dprob(problem)
-    n = int(lib().cosa_decode_workspace_bytes(ctypes.byref(p)))
+    n = int(lib().cosa_decode_workspace_bytes(p))
     if n == 0:
         raise CosaError(COSA_ERR_INVALID_ARG, cosa_last_error())
     return n
@@ -576,27 +597,24 @@ def cosa_decode_workspace_bytes(problem) -> int:
 
 def cosa_decode_attention(problem, q, kv: CosaPagedKv, seq_lens, workspace, workspace_bytes: int, o,
                           lse=None, stream=None):
-    s = _decode_stream(stream, q, seq_lens, workspace, o, lse)
-    p, qp = _dprob(problem, q)
-    _check(lib().cosa_decode_attention(ctypes.byref(p), qp, _kvref(kv), _ptr(seq_lens),
-                                       _ptr(workspace), workspace_bytes, _ptr(o), _ptr(lse), s))
+    s, (lens, ws, out, ls) = _place(stream, seq_lens, workspace, o, lse)
+    p, qp = _dprob(problem, q, o)
+    _check(lib().cosa_decode_attention(p, qp, _kvref(kv), lens, ws, workspace_bytes, out, ls, s))
 
 
 def cosa_decode_attention_listed(problem, q, kv: CosaPagedKv, seq_lens, pages, count,
                                  list_pages: int, workspace, workspace_bytes: int, o, lse=None,
                                  stream=None):
-    s = _decode_stream(stream, q, seq_lens, pages, count, workspace, o, lse)
-    p, qp = _dprob(problem, q)
-    _check(lib().cosa_decode_attention_listed(ctypes.byref(p), qp, _kvref(kv), _ptr(seq_lens),
-                                              _ptr(pages), _ptr(count), list_pages, _ptr(workspace),
-                                              workspace_bytes, _ptr(o), _ptr(lse), s))
+    s, (lens, pg, cnt, ws, out, ls) = _place(stream, seq_lens, pages, count, workspace, o, lse)
+    p, qp = _dprob(problem, q, o)
+    _check(lib().cosa_decode_attention_listed(p, qp, _kvref(kv), lens, pg, cnt, list_pages, ws,
+                                              workspace_bytes, out, ls, s))
 
 
 def cosa_decode_sparse_workspace_layout(problem, budget: CosaPageBudget) -> CosaDecodeSparseLayout:
     p, _ = _dprob(problem)
     out = CosaDecodeSparseLayout()
-    _check(lib().cosa_decode_sparse_workspace_layout(ctypes.byref(p), _kvref(budget),
-                                                     ctypes.byref(out)))
+    _check(lib().cosa_decode_sparse_workspace_layout(p, _kvref(budget), ctypes.byref(out)))
     return out
 
 
@@ -606,8 +624,7 @@ def cosa_decode_sparse_workspace_bytes(problem, budget: CosaPageBudget) -> int:
 
 def cosa_decode_sparse(problem, q, kv: CosaPagedKv, bounds, seq_lens, budget: CosaPageBudget,
                        workspace, workspace_bytes: int, o, lse=None, stream=None):
-    s = _decode_stream(stream, q, bounds, seq_lens, workspace, o, lse)
-    p, qp = _dprob(problem, q)
-    _check(lib().cosa_decode_sparse(ctypes.byref(p), qp, _kvref(kv), _ptr(bounds), _ptr(seq_lens),
-                                    _kvref(budget), _ptr(workspace), workspace_bytes, _ptr(o),
-                                    _ptr(lse), s))
+    s, (b, lens, ws, out, ls) = _place(stream, bounds, seq_lens, workspace, o, lse)
+    p, qp = _dprob(problem, q, o)
+    _check(lib().cosa_decode_sparse(p, qp, _kvref(kv), b, lens, _kvref(budget), ws, workspace_bytes,
+                                    out, ls, s))

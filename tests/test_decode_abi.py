@@ -1,6 +1,7 @@
 """Host-side checks of the decode entry points that need no GPU: declared and exported symbols, refusals
 before anything is enqueued, workspace layout, and what the binding refuses."""
 import ctypes
+import dataclasses
 import subprocess
 
 import pytest
@@ -22,7 +23,7 @@ def kv(page=64, n_pages=16, k=16, v=16, table=16):
 
 
 def change(**kw):
-    return B.DecodeProblem(**{**GOOD.__dict__, **kw})
+    return dataclasses.replace(GOOD, **kw)
 
 
 CALLS = {
@@ -183,18 +184,15 @@ def test_binding_refuses_cpu_tensors_and_overlapping_rows():
     with pytest.raises(ValueError):
         B.cosa_page_score(GOOD, q, kv(), 16, 16, 16, stream=0)
 
-    class Cuda:  # what _rows asks of a tensor
-        is_cuda = True
+    class Cuda:  # a tensor that says it lives on a GPU
+        def __init__(self, t, device=0):
+            self.t, self.device_index = t, device
 
-        def __init__(self, t):
-            self.t = t
-            self.shape = t.shape
+        def get_device(self):
+            return self.device_index
 
         def __getattr__(self, name):
             return getattr(self.t, name)
-
-        def __getitem__(self, i):
-            return self.t[i]
     wide = torch.zeros(4, 24, 128, dtype=torch.bfloat16)
     assert B._rows(Cuda(wide[:, 4:12]), 0)[1] == 24 * 128
     assert B._rows(Cuda(wide[:1, 4:12]), 0)[1] == 8 * 128
@@ -205,3 +203,12 @@ def test_binding_refuses_cpu_tensors_and_overlapping_rows():
             B._rows(Cuda(bad), 0)
     with pytest.raises(ValueError):
         B._rows(Cuda(wide), 8)
+    # one device for all tensors, and its stream
+    one, other = Cuda(wide), Cuda(wide, 1)
+    assert B._place(0, one, None, 7, one)[1] == [wide.data_ptr(), None, 7, wide.data_ptr()]
+    with pytest.raises(ValueError):
+        B._place(0, one, other)
+    with pytest.raises(ValueError):
+        B._place(0, one, Cuda(wide[:, ::2]))
+    with pytest.raises(ValueError):
+        B._rows(one, 0, other)
