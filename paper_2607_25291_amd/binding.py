@@ -508,7 +508,10 @@ def _device(t, device: Optional[int]) -> int:
 def _stream_of(stream, device: Optional[int]) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream(device).cuda_stream
+        if device is None:
+            return torch.cuda.current_stream().cuda_stream
+        # the handle alone: torch.cuda.current_stream() takes 1 us to build a Stream around it
+        return torch._C._cuda_getCurrentRawStream(device)
     if isinstance(stream, int):
         return stream
     if device is not None and stream.device.index != device:

@@ -15,19 +15,17 @@
 // a second kernel joins them in order.
 //
 // Bound: HBM. A token costs 512 bytes per KV head and 4 G d flops, G flops per byte.
-#include "cosa_device.h"
+#include "decode_device.h"
 #include "decode_internal.h"
 #include "select_wave.h"
 
 namespace cosa {
 namespace {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-constexpr int kThreads = 256, kWaves = 4;
-constexpr int kTile = 128;     // tokens of a tile: 32 per wave
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr int kTile = 32 * kWaves;  // tokens of a tile: 32 per wave
 constexpr int kGrid = 512;     // workgroups that share the tiles: two per CU
-constexpr int kWholeTiles = 4; // units of at most this many tiles are not split
+
 constexpr int kRows = 16;      // query heads of a unit
 constexpr int kPartStride = kRows * (kHeadDim + 2);  // floats of a partial result
 
@@ -35,7 +33,7 @@ struct DecodeParams {
   const uint16_t *q, *kc, *vc;
   const int32_t *table, *seq_lens, *pages, *count;
   float* part;    // [2 * grid][kPartStride]: the partial results of a workgroup's first and last unit
-  int2* rec;      // [grid]: the unit that starts in a workgroup and goes on behind it, and the last workgroup it reaches
+  int2* rec;      // [units]: first and last workgroup of a unit that several share; first < 0: one had it all
   uint16_t* o;
   float* lse;
   int Hq, Hkv, G, QG;
@@ -44,10 +42,6 @@ struct DecodeParams {
   long long q_stride, n_pages;
   float scale_log2;
 };
-
-__device__ __forceinline__ f32x4_t mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4_t& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
-}
 
 __device__ __forceinline__ float xmax16(float v) { return fmaxf(v, __shfl_xor(v, 16, 64)); }
 
@@ -74,6 +68,12 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint3
   const float ra = a - __uint_as_float(hi << 16), rb = b - __uint_as_float(hi & 0xffff0000u);
   lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{ra, rb}), bf16x2_t));
 }
+
+// Rows of the cache as a buffer that ends behind `bytes`.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint16_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
+}
+constexpr int kOnce = 2;  // cache policy of a buffer load: read once (ldg16_once)
 
 struct Tile {
   u32x4_t k[2][4], v[8];
@@ -105,7 +105,8 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
   const int32_t* row = P.table + (size_t)n * P.max_pages;
   const int32_t* list = LISTED ? P.pages + (size_t)(n * P.Hkv + g) * P.list_pages : nullptr;
 
-  // Pages of steps i0 .. i0 + 63, one per lane: physical page and valid keys of either half.
+  // Pages of steps i0 .. i0 + 63, one per lane: physical page and valid keys of either half (behind the last step:
+  // none).
   int pg[2], valid[2];
   const auto look_up = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
@@ -126,19 +127,29 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
       }
     }
   };
-  const auto load = [&](Tile& T, int i) __attribute__((always_inline)) {
+  // Keys of lane-step i and of half h that count (none behind the 64 steps that were looked up).
+  const auto keys_of = [&](int i, int h) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readlane(valid[h], i & 63) & ((i - 64) >> 31);
+  };
+  // The loads of a step are never branched around, so that they can stay in flight over the step before: a buffer of
+  // as many rows as count gives zeros, and reads nothing, behind them.
+  const auto load = [&](Tile& T, unsigned pos, int i) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);  // one step's loads follow another's, as the waits count them
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const unsigned pos = begin + (unsigned)i * kTile + h * 16;
       const size_t p = (size_t)(unsigned)__builtin_amdgcn_readlane(pg[h], i & 63);
-      const size_t at = (((p * P.Hkv + g) << P.log2_page) + (pos & (unsigned)(page - 1))) * kHeadDim;
-      const uint16_t* kp = P.kc + at;
-      const uint16_t* vp = P.vc + at;
+      const size_t at = (((p * P.Hkv + g) << P.log2_page) + ((pos + h * 16) & (unsigned)(page - 1))) * kHeadDim;
+      const int bytes = keys_of(i, h) * (kHeadDim * 2);
+      const __amdgpu_buffer_rsrc_t kr = buffer_of(P.kc + at, bytes), vr = buffer_of(P.vc + at, bytes);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) T.k[h][c] = ldg16(kp + (r * kHeadDim + c * 32 + gq * 8));
+      for (int c = 0; c < 4; ++c)
+        T.k[h][c] = __builtin_amdgcn_raw_buffer_load_b128(kr, r * (kHeadDim * 2) + gq * 16 + c * 64, 0, 0);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) T.v[h * 4 + c] = ldg16(vp + ((gq * 4 + c) * kHeadDim + r * 8));
+      for (int c = 0; c < 4; ++c)
+        T.v[h * 4 + c] =
+            __builtin_amdgcn_raw_buffer_load_b128(vr, gq * 4 * (kHeadDim * 2) + r * 16 + c * (kHeadDim * 2), 0, kOnce);
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
   const auto compute = [&](Tile& T, int v0, int v1) __attribute__((always_inline)) {
     f32x4_t s[2];
@@ -148,15 +159,12 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[h] = mfma16(T.k[h][c], qf[c], s[h]);
     }
-    if (v0 < 16 || v1 < 16) {  // keys behind the sequence: no weight, and values that cannot spoil the sum
+    if (v0 < 16 || v1 < 16) {  // keys behind the sequence (read as zeros, as their values are): no weight
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (gq * 4 + i >= (h ? v1 : v0)) {
-            s[h][i] = -INFINITY;
-            T.v[h * 4 + i] = u32x4_t{0, 0, 0, 0};
-          }
+          if (gq * 4 + i >= (h ? v1 : v0)) s[h][i] = -INFINITY;
     }
     float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
@@ -199,23 +207,24 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
     }
   };
 
-  if (steps > 0) {
+  for (int i0 = 0; i0 < steps; i0 += 64) {
+    const int n_steps = min(steps - i0, 64);
+    const unsigned pos = begin + (unsigned)i0 * kTile;
     Tile A, B;
-    look_up(0);
-    load(A, 0);
-    for (int i = 0; i < steps; i += 2) {
-      int v0 = __builtin_amdgcn_readlane(valid[0], i & 63), v1 = __builtin_amdgcn_readlane(valid[1], i & 63);
-      if (i + 1 < steps) load(B, i + 1);
-      const int b0 = __builtin_amdgcn_readlane(valid[0], (i + 1) & 63);
-      const int b1 = __builtin_amdgcn_readlane(valid[1], (i + 1) & 63);
-      if (((i + 2) & 63) == 0) look_up(i + 2);
-      compute(A, v0, v1);
-      if (i + 2 < steps) load(A, i + 2);
-      if (i + 1 < steps) compute(B, b0, b1);
+    look_up(i0);
+    load(A, pos, 0);
+    load(B, pos + kTile, 1);
+    int i = 0;
+    for (; i + 1 < n_steps; i += 2) {
+      compute(A, keys_of(i, 0), keys_of(i, 1));
+      load(A, pos + (unsigned)(i + 2) * kTile, i + 2);
+      compute(B, keys_of(i + 1, 0), keys_of(i + 1, 1));
+      load(B, pos + (unsigned)(i + 3) * kTile, i + 3);
     }
+    if (i < n_steps) compute(A, keys_of(i, 0), keys_of(i, 1));
   }
 
-  // The four waves' results: lane (r, gq) holds columns d = 8 (4 gq + i) + e of query head r.
+  // The waves' results: lane (r, gq) holds columns d = 8 (4 gq + i) + e of query head r.
   l += __shfl_xor(l, 16, 64);
   l = half_sum(l);
   if (r < rows) {
@@ -260,6 +269,21 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
   __syncthreads();  // so, sm and sl are used again
 }
 
+// Tiles [begin, end) of workgroup w of n, of `all` tiles: the first all % n workgroups have one more than the others.
+struct Range {
+  uint32_t begin, end;
+};
+__device__ __forceinline__ Range range_of(uint32_t w, uint32_t n, uint32_t all) {
+  const uint32_t q = all / n, r = all % n;
+  const uint32_t begin = w * q + min(w, r);
+  return {begin, begin + q + (w < r)};
+}
+// The workgroup whose range holds tile x.
+__device__ __forceinline__ int owner_of(uint32_t x, uint32_t n, uint32_t all) {
+  const uint32_t q = all / n, r = all % n, big = r * (q + 1);
+  return (int)(x < big ? x / (q + 1) : r + (x - big) / q);
+}
+
 // WHOLE: a workgroup per unit, no splitting.
 template <bool LISTED, bool WHOLE>
 __global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
@@ -275,54 +299,65 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
     unit(item, blockIdx.x % P.mult, 0, tiles_of(tokens), tokens, nullptr);
     return;
   }
-  __shared__ uint32_t waves[kWaves];
-  __shared__ int found[2];
+  // Tiles of the items before each lane's share of them, and all tiles.
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  // Tiles of the items before each thread's share of them, and all tiles.
-  const int per = (P.items + kThreads - 1) / kThreads;
-  const int i0 = min((int)threadIdx.x * per, P.items), i1 = min(i0 + per, P.items);
-  uint32_t sum = 0;
-  for (int i = i0; i < i1; ++i) sum += (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
-  const uint32_t incl = wave_incl_scan(sum, lane);
-  if (lane == 63) waves[w] = incl;
-  __syncthreads();
-  uint32_t at = incl - sum, total = 0;
+  uint32_t total, before;  // all tiles; tiles in front of the item
+  int item;
+  Range R;
+  if (P.items <= 64) {  // one item a lane: every wave for itself
+    const uint32_t t = lane < P.items ? (uint32_t)tiles_of(item_tokens<LISTED>(P, lane)) : 0u;
+    const uint32_t at = wave_incl_scan(t, lane) - t;
+    total = __builtin_amdgcn_readlane(at + t, 63);
+    R = range_of(blockIdx.x, gridDim.x, total * P.mult);
+    item = __builtin_popcountll(__ballot(lane < P.items && at <= R.begin / (uint32_t)P.mult)) - 1;
+    before = __builtin_amdgcn_readlane(at, item);
+  } else {
+    __shared__ uint32_t waves[kWaves];
+    __shared__ int found[2];
+    const int per = (P.items + kThreads - 1) / kThreads;
+    const int i0 = min((int)threadIdx.x * per, P.items), i1 = min(i0 + per, P.items);
+    uint32_t sum = 0;
+    for (int i = i0; i < i1; ++i) sum += (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+    const uint32_t incl = wave_incl_scan(sum, lane);
+    if (lane == 63) waves[w] = incl;
+    __syncthreads();
+    uint32_t at = incl - sum;
+    total = 0;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < w) at += waves[i];
-    total += waves[i];
-  }
-  const uint64_t W = (uint64_t)total * P.mult;
-  const uint64_t N = W < gridDim.x ? W : gridDim.x;
-  if (threadIdx.x == 0) P.rec[blockIdx.x] = int2{-1, 0};
-  if (blockIdx.x >= N) return;
-  uint64_t a = blockIdx.x * W / N;
-  const uint64_t b = (blockIdx.x + 1) * W / N;
-  const uint32_t x = (uint32_t)(a / P.mult);
-  if (x >= at && x < at + sum) {
-    int i = i0;
-    for (;; ++i) {
-      const uint32_t t = (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
-      if (x < at + t) break;
-      at += t;
+    for (int i = 0; i < kWaves; ++i) {
+      if (i < w) at += waves[i];
+      total += waves[i];
     }
-    found[0] = i;
-    found[1] = (int)at;
+    R = range_of(blockIdx.x, gridDim.x, total * P.mult);
+    const uint32_t x = R.begin / (uint32_t)P.mult;
+    if (x >= at && x < at + sum) {
+      int i = i0;
+      for (;; ++i) {
+        const uint32_t t = (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+        if (x < at + t) break;
+        at += t;
+      }
+      found[0] = i;
+      found[1] = (int)at;
+    }
+    __syncthreads();
+    item = __builtin_amdgcn_readfirstlane(found[0]);
+    before = __builtin_amdgcn_readfirstlane(found[1]);
   }
-  __syncthreads();
-  int item = __builtin_amdgcn_readfirstlane(found[0]);
+  uint32_t a = R.begin;
+  const uint32_t b = R.end;
+  if (a == b) return;
   int tokens = item_tokens<LISTED>(P, item);
   int tiles = tiles_of(tokens);
-  const uint32_t rem = (uint32_t)(a - (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(found[1]) * P.mult);
+  const uint32_t rem = a - before * P.mult;
   int sub = (int)(rem / (uint32_t)tiles), t0 = (int)(rem % (uint32_t)tiles);
   for (;;) {
-    const int t1 = (int)(b - a < (uint64_t)(tiles - t0) ? t0 + (b - a) : tiles);
+    const int t1 = (int)min((uint32_t)t0 + (b - a), (uint32_t)tiles);
     float* part = nullptr;
     if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride;
-    if (t0 == 0 && t1 < tiles && threadIdx.x == 0) {
-      const uint64_t end = a + tiles;  // behind the unit's last tile
-      P.rec[blockIdx.x] = int2{item * P.mult + sub, (int)((end * N - 1) / W)};
-    }
+    if (t0 == 0 && threadIdx.x == 0)
+      P.rec[item * P.mult + sub] =
+          t1 < tiles ? int2{(int)blockIdx.x, owner_of(a + tiles - 1, gridDim.x, total * P.mult)} : int2{-1, 0};
     unit(item, sub, t0, t1, tokens, part);
     a += t1 - t0;
     if (a >= b) return;
@@ -335,44 +370,75 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
   }
 }
 
-// Joins the partial results of the unit that starts in workgroup blockIdx.x and goes on behind it, query head
-// blockIdx.y of the unit.
+constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
+
+// Joins the partial results of unit blockIdx.x, for `heads` query heads from blockIdx.y * heads on. A group of 32 threads adds partial results, four columns a
+// thread; the 16 groups are dealt to the heads and, within a head, to its partial results in turn, so that
+// the loads of many wait side by side.
 template <bool LISTED>
-__global__ __launch_bounds__(kHeadDim) void join_kernel(DecodeParams P) {
-  __shared__ float red[2];
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int heads, int log2_per_head) {
+  __shared__ f32x4_t sums[kJoinGroups][32];
+  __shared__ float lsum[kJoinGroups], tops[kJoinGroups];
   const int2 rec = P.rec[blockIdx.x];
   if (rec.x < 0) return;
-  const int item = rec.x / P.mult, sub = rec.x % P.mult;
+  const int item = blockIdx.x / P.mult, sub = blockIdx.x % P.mult;
   const int n = LISTED ? item / P.Hkv : item, g = LISTED ? item % P.Hkv : sub / P.QG, qg = sub % P.QG;
-  const int hh = blockIdx.y, d = threadIdx.x;
-  if (qg * kRows + hh >= P.G) return;
-  const int first = blockIdx.x, n_parts = rec.y - first + 1;
+  const int t = threadIdx.x & 31, group = threadIdx.x >> 5;
+  const int per_head = 1 << log2_per_head, mine = group & (per_head - 1);
+  const int slot = group >> log2_per_head, hh = blockIdx.y * heads + slot;
+  const bool live = slot < heads && qg * kRows + hh < P.G;
+  const int first = rec.x, n_parts = rec.y - first + 1;
   const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * kPartStride; };
-  float M = -INFINITY;
-  for (int i = d; i < n_parts; i += kHeadDim) M = fmaxf(M, part(i)[kRows * kHeadDim + hh]);
-  M = wave_max(M);
-  if ((d & 63) == 0) red[d >> 6] = M;
-  __syncthreads();
-  M = fmaxf(red[0], red[1]);
-  const float base = M == -INFINITY ? 0.f : M;
-  float L = 0.f, O = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < n_parts; ++i) {
-    const float* p = part(i);
-    const float a = __builtin_amdgcn_exp2f(p[kRows * kHeadDim + hh] - base);
-    L += a * p[kRows * (kHeadDim + 1) + hh];
-    O += a * p[hh * kHeadDim + d];
+  float M = -INFINITY, L = 0.f;
+  f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+  const auto add = [&](float m, float l, const f32x4_t& o) {
+    const float mx = fmaxf(M, m), base = mx == -INFINITY ? 0.f : mx;
+    const float a = __builtin_amdgcn_exp2f(M - base), b = __builtin_amdgcn_exp2f(m - base);
+    L = a * L + b * l;
+    O = a * O + b * o;
+    M = mx;
+  };
+  if (live) {
+    for (int i0 = mine; i0 < n_parts; i0 += 4 * per_head) {
+      float m[4], l[4];
+      f32x4_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // behind the last part: that one again, without weight
+        const float* p = part(min(i0 + i * per_head, n_parts - 1));
+        m[i] = p[kRows * kHeadDim + hh];
+        l[i] = p[kRows * (kHeadDim + 1) + hh];
+        o[i] = *reinterpret_cast<const f32x4_t*>(p + hh * kHeadDim + t * 4);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i0 + i * per_head < n_parts) add(m[i], l[i], o[i]);
+    }
+    sums[group][t] = O;
+    if (t == 0) {
+      lsum[group] = L;
+      tops[group] = M;
+    }
   }
+  __syncthreads();
+  if (!live || mine != 0) return;
+  for (int i = 1; i < per_head; ++i) add(tops[group + i], lsum[group + i], sums[group + i][t]);
   const size_t out = (size_t)n * P.Hq + (size_t)g * P.G + qg * kRows + hh;
-  const __bf16 v = (__bf16)(M == -INFINITY ? 0.f : O / L);
-  P.o[out * kHeadDim + d] = __builtin_bit_cast(uint16_t, v);
-  if (P.lse && d == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
+  uint16_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint16_t, (__bf16)(M == -INFINITY ? 0.f : O[i] / L));
+  *reinterpret_cast<u32x2_t*>(P.o + out * kHeadDim + t * 4) =
+      u32x2_t{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
+  if (P.lse && t == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
 }
 
 template <bool LISTED>
 hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream) {
   const long long units = (long long)P.items * P.mult, tiles = (tokens + kTile - 1) / kTile;
-  if (tiles <= kWholeTiles) {
+  // A workgroup for every unit, and no join, where a unit is short, or less short and there are enough of them: 8
+  // units of 256 / 512 / 1000 tokens 11.6 / 13.7 / 18.0 us (split 15.0 / 15.4 / 15.5); 256 units of 512 / 1000 / 2000
+  // 18.7 / 28.0 / 46.4 (23.5 / 32.2 / 50.0), 320 of them 24.9 / 38.3 / 71.3 (26.8 / 38.5 / 67.0), 800 of them 42.4 /
+  // 80.7 / 150 (45.1 / 80.6 / 148).
+  if (tokens <= 512 || (tokens <= 1024 && units >= 256)) {
     hipLaunchKernelGGL((decode_kernel<LISTED, true>), dim3((unsigned)units), dim3(kThreads), 0, stream, P);
     return hipGetLastError();
   }
@@ -380,14 +446,26 @@ hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream)
   hipLaunchKernelGGL((decode_kernel<LISTED, false>), dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((join_kernel<LISTED>), dim3(grid, std::min(P.G, kRows)), dim3(kHeadDim), 0, stream, P);
+  // Few units leave many partial results each: then every head has workgroups of its own.
+  const int rows = std::min(P.G, kRows), parts = (int)std::min<long long>(std::max<long long>(256 / units, 1), rows);
+  const int heads = (rows + parts - 1) / parts;
+  int log2_per_head = 4;
+  while (heads << log2_per_head > kJoinGroups) --log2_per_head;
+  hipLaunchKernelGGL((join_kernel<LISTED>), dim3((unsigned)units, (rows + heads - 1) / heads), dim3(kJoinThreads), 0, stream, P,
+                     heads, log2_per_head);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t decode_workspace_bytes(const DecodeShape&) {
-  return ((size_t)kGrid * sizeof(int2) + 255) / 256 * 256 + (size_t)kGrid * 2 * kPartStride * sizeof(float);
+// The workspace: a record per unit, then two partial results per workgroup.
+static size_t record_bytes(const DecodeShape& sh) {
+  const size_t units = (size_t)sh.B * sh.Hkv * ((sh.G + kRows - 1) / kRows);
+  return (units * sizeof(int2) + 255) / 256 * 256;
+}
+
+size_t decode_workspace_bytes(const DecodeShape& sh) {
+  return record_bytes(sh) + (size_t)kGrid * 2 * kPartStride * sizeof(float);
 }
 
 bool decode_fits(const DecodeShape& sh, long long tokens) {
@@ -398,7 +476,7 @@ bool decode_fits(const DecodeShape& sh, long long tokens) {
 hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream) {
   const int QG = (sh.G + kRows - 1) / kRows;
   int2* rec = static_cast<int2*>(a.workspace);
-  float* part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + ((size_t)kGrid * sizeof(int2) + 255) / 256 * 256);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + record_bytes(sh));
   const bool listed = a.pages != nullptr;
   const DecodeParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.pages, a.count, part, rec, a.o, a.lse,
                        sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages, sh.log2_page, a.list_pages,

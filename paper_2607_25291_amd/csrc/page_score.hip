@@ -4,42 +4,34 @@
 // cores, rows the pages and columns the query heads of one KV head (16 of them). Each lane reads its
 // operands straight from the bounds: 512 contiguous bytes per (page, KV head), which are also all the
 // bytes there are to read, so HBM bounds it.
-#include "cosa_device.h"
+#include "decode_device.h"
 #include "decode_internal.h"
 
 namespace cosa {
 namespace {
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
 struct ScoreParams {
   const uint16_t *q, *bounds;
   const int32_t *table, *seq_lens;
   float* score;
-  int Hq, Hkv, G, QG, max_pages, log2_page, segs, n_waves;  // segs: waves along a row of pages
+  int Hq, Hkv, G, QG, max_pages, log2_page, segs;  // segs: waves along a row of pages
   long long q_stride, n_pages;
   float scale;
+  bool wide;  // rows of scores start on 16 bytes
 };
 
-// D (16 x 16, fp32) = A (16 x 32) B (32 x 16) + C, bf16: lane l supplies row / column l % 16 and k = 8 (l / 16)
-// .. + 7; D row 4 (l / 16) + i, column l % 16 in register i.
-__device__ __forceinline__ f32x4_t mfma16(const u32x4_t& a, const u32x4_t& b, const f32x4_t& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
-}
-
-// A wave scores TILES groups of 16 pages. Waves that follow each other take the KV heads of the same pages, so that a
-// page's bounds, contiguous over its heads, are read at about one time. Lengths, table entries and queries
-// are loaded side by side: a table entry is read before it is known to be in use.
-template <int TILES>
-__global__ __launch_bounds__(256) void page_score_kernel(ScoreParams P) {
-  const int lane = threadIdx.x & 63, r = lane & 15, gq = lane >> 4;
-  const int id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (id >= P.n_waves) return;
+// A wave scores 16 pages. Waves that follow each other take the KV heads of the same pages, so that a page's
+// bounds, contiguous over its heads, are read at about one time. Lengths, table entries and queries are loaded
+// side by side: a table entry is read before it is known to be in use.
+template <bool ONCE>
+__global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
+  const int lane = threadIdx.x, r = lane & 15, gq = lane >> 4;
+  const int id = blockIdx.x;
   const int hq = id % (P.Hkv * P.QG), g = hq / P.QG, qg = hq % P.QG;
   const int ns = id / (P.Hkv * P.QG), n = ns / P.segs;
-  const int j0 = (ns % P.segs) * (TILES * 16);
+  const int j0 = (ns % P.segs) * 16;
   const int32_t* row = P.table + (size_t)n * P.max_pages;
-  long long p = j0 + lane < P.max_pages && lane < TILES * 16 ? row[j0 + lane] : 0;
+  long long p = j0 + r < P.max_pages ? row[j0 + r] : 0;
   const int page = 1 << P.log2_page;
   const int len = min(max(P.seq_lens[n], 0), P.max_pages << P.log2_page);
   const int np = (int)(((unsigned)len + page - 1) >> P.log2_page);
@@ -62,31 +54,26 @@ __global__ __launch_bounds__(256) void page_score_kernel(ScoreParams P) {
   const int page_of_lane = (int)p;
   const bool stores = qg * 16 + r < P.G;
   float* out = P.score + ((size_t)n * P.Hq + h) * P.max_pages;
+  RowOperands<4, ONCE> x;  // minimum, then maximum
+  x.load(lane, [&](int k) __attribute__((always_inline)) {
+    const size_t pg = (unsigned)__shfl(page_of_lane, k, 64);
+    return P.bounds + (pg * P.Hkv + g) * 2 * kHeadDim;
+  });
+  x.to_operands();
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < TILES; ++i) {
-    const int j = j0 + i * 16;
-    if (j >= np) break;
-    const size_t pg = (unsigned)(TILES == 1 ? __shfl(page_of_lane, r, 64) : __shfl(page_of_lane, i * 16 + r, 64));
-    const uint16_t* b = P.bounds + (pg * P.Hkv + g) * 2 * kHeadDim + gq * 8;
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < 4; ++c) acc = mfma16(x.x[c], qm[c], acc);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc = mfma16(ldg16(b + c * 32), qm[c], acc);
+  for (int c = 0; c < 4; ++c) acc = mfma16(x.x[4 + c], qp[c], acc);
+  if (!stores) return;
+  out += j0 + gq * 4;
+  if (P.wide && j0 + gq * 4 + 3 < np) {
+    *reinterpret_cast<f32x4_t*>(out) = acc * P.scale;
+  } else {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) acc = mfma16(ldg16(b + kHeadDim + c * 32), qp[c], acc);
-    if (stores) {
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (j + gq * 4 + v < np) out[j + gq * 4 + v] = acc[v] * P.scale;
-    }
+    for (int v = 0; v < 4; ++v)
+      if (j0 + gq * 4 + v < np) out[v] = acc[v] * P.scale;
   }
-}
-
-template <int TILES>
-hipError_t launch_t(ScoreParams P, int B, hipStream_t stream) {
-  P.segs = (P.max_pages + TILES * 16 - 1) / (TILES * 16);
-  P.n_waves = B * P.segs * P.Hkv * P.QG;
-  hipLaunchKernelGGL((page_score_kernel<TILES>), dim3((P.n_waves + 3) / 4), dim3(256), 0, stream, P);
-  return hipGetLastError();
 }
 
 }  // namespace
@@ -95,10 +82,18 @@ hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uin
                              const int32_t* table, const int32_t* seq_lens, float* score,
                              hipStream_t stream) {
   const int QG = (sh.G + 15) / 16;
+  const int segs = (sh.max_pages + 15) / 16, n_waves = sh.B * segs * sh.Hkv * QG;
   const ScoreParams P{q, bounds, table, seq_lens, score, sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages,
-                      sh.log2_page, 0, 0, sh.q_stride, sh.n_pages, sh.scale};
-  return (long long)sh.B * sh.Hkv * QG * ((sh.max_pages + 63) / 64) >= 4096 ? launch_t<4>(P, sh.B, stream)
-                                                                            : launch_t<1>(P, sh.B, stream);
+                      sh.log2_page, segs, sh.q_stride, sh.n_pages, sh.scale,
+                      sh.max_pages % 4 == 0 && reinterpret_cast<uintptr_t>(score) % 16 == 0};
+  // Bounds that fit the 256 MB of the last-level cache may still be there from the step before: plain loads keep
+  // them (75 MB: 23.4 us, 25.2 with loads that do not). Larger ones only push others out (307 MB: 76.9 us
+  // and 74.7).
+  if (sh.n_pages * sh.Hkv * (4 * kHeadDim) <= 256ll << 20)
+    hipLaunchKernelGGL((page_score_kernel<false>), dim3(n_waves), dim3(64), 0, stream, P);
+  else
+    hipLaunchKernelGGL((page_score_kernel<true>), dim3(n_waves), dim3(64), 0, stream, P);
+  return hipGetLastError();
 }
 
 }  // namespace cosa
