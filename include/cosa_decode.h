@@ -120,7 +120,7 @@ cosa_status cosa_page_score(const cosa_decode_problem* problem, const void* q,
  * recent pages are kept, then the pages of largest s, ties by ascending j, up to K (cosa_page_budget).
  * pages int32 [batch, n_kv_heads, budget->max_pages]: the kept pages in ascending order, then -1;
  * count int32 [batch, n_kv_heads] = K (0 for an empty sequence). A NaN difference counts as the largest; the
- * row maximum passes over NaN scores. max_pages <= 32768.
+ * row maximum passes over NaN scores. max_pages <= 32768, at most 1024 query heads per KV head.
  */
 cosa_status cosa_page_select(const cosa_decode_problem* problem, int32_t page_size,
                              const int32_t* seq_lens, const float* score,

@@ -126,9 +126,9 @@ cosa_status check_budget(const cosa_page_budget* b, int64_t& micro) {
 }
 
 cosa_status check_select_space(const DecodeShape& sh) {
-  if (sh.max_pages > cosa::kMaxSelectPages || sh.G > 4096)
-    return fail(COSA_ERR_UNSUPPORTED, "%d pages and %d query heads per KV head (supported: <= %d and 4096)", sh.max_pages,
-                sh.G, cosa::kMaxSelectPages);
+  if (sh.max_pages > cosa::kMaxSelectPages || sh.G > cosa::kMaxSelectHeads)
+    return fail(COSA_ERR_UNSUPPORTED, "%d pages and %d query heads per KV head (supported: <= %d and %d)", sh.max_pages,
+                sh.G, cosa::kMaxSelectPages, cosa::kMaxSelectHeads);
   return ok();
 }
 

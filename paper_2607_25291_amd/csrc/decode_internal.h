@@ -12,6 +12,7 @@ namespace cosa {
 
 constexpr int kMaxRequests = 8192;      // requests of one cosa_page_map (two prefix arrays in LDS)
 constexpr int kMaxSelectPages = 32768;  // pages of one row of cosa_page_select (32-bit keys in LDS)
+constexpr int kMaxSelectHeads = 1024;   // query heads of one KV head there
 
 // A validated decode problem with its cache.
 struct DecodeShape {

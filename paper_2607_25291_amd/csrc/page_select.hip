@@ -5,6 +5,10 @@
 // pages, NaN, then descending s). A radix selection finds the K-th largest key and how many pages that
 // equal it are kept; a scan over the pages then packs the kept ones in ascending order, so the list needs
 // no sort.
+//
+// Bound: latency (the barriers between its steps). 256 rows of up to 4096 pages, 7 heads: 12.1 us for 8.7 MB; 8 rows
+// of 256 pages, 4 heads: 5.9 us, of which an empty launch takes 2. Comparing all pairs of 256 keys instead of
+// the radix selection: 14.2 us.
 #include <mutex>
 
 #include "cosa_device.h"
@@ -22,23 +26,29 @@ __device__ __forceinline__ uint32_t key_of(float s) {
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// Scores of one head at pages j, j + T, j + 2 T, j + 3 T (-inf behind the row).
-template <int T>
-__device__ __forceinline__ void load4(float (&x)[4], const float* row, int j, int np) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = j + i * T < np ? row[j + i * T] : -INFINITY;
-}
-
 constexpr int kBins = 2048;
 
-template <int T>
+// Scores of kHeads heads from h0 on (the last one again behind G) at pages j, j + T, j + 2 T, j + 3 T (-inf behind the
+// row).
+template <int T, int kHeads>
+__device__ __forceinline__ void load_scores(float (&x)[kHeads][4], const PageSelectArgs& A, const float* score, int h0,
+                                            int j, int np) {
+#pragma unroll
+  for (int k = 0; k < kHeads; ++k) {
+    const float* row = score + (size_t)min(h0 + k, A.G - 1) * A.max_pages;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[k][i] = j + i * T < np ? row[j + i * T] : -INFINITY;
+  }
+}
+
+template <int T, int kHeads>
 __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
   constexpr int kWaves = T / 64, kPer = kBins / T;
-  extern __shared__ uint32_t lds[];
+  extern __shared__ __align__(16) uint32_t lds[];
   uint32_t* keys = lds;                                                       // max_pages, in fours
-  float* top = reinterpret_cast<float*>(lds + (A.max_pages + 3) / 4 * 4);     // row maxima of the group's heads
-  __shared__ uint32_t hist[kBins], waves[kWaves], pick[3];
-  __shared__ float part[4][kWaves];
+  float* top = reinterpret_cast<float*>(lds + (A.max_pages + 3) / 4 * 4);     // row maxima of the group's heads, in kHeads
+  __shared__ uint32_t hist[3][kBins], waves[kWaves], pick[3];
+  __shared__ float part[kHeads][kWaves];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int u = blockIdx.x, n = u / A.Hkv, g = u % A.Hkv;
   const int page = 1 << A.log2_page;
@@ -54,38 +64,41 @@ __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
     return;
   }
   const float* score = A.score + ((size_t)n * A.Hq + (size_t)g * A.G) * A.max_pages;
-  // Row maxima, four heads at a time.
-  for (int h0 = 0; h0 < A.G; h0 += 4) {
-    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  for (int i = threadIdx.x; i < kBins; i += T) hist[0][i] = 0;
+  // Row maxima, kHeads at a time. Up to so many heads of 4 T pages stay in registers for the keys.
+  float x[kHeads][4];
+  for (int h0 = 0; h0 < A.G; h0 += kHeads) {
+    float m[kHeads];
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) m[k] = -INFINITY;
     for (int j = threadIdx.x; j < np; j += 4 * T) {
-      float x[4][4];
+      load_scores<T, kHeads>(x, A, score, h0, j, np);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) load4<T>(x[k], score + (size_t)min(h0 + k, A.G - 1) * A.max_pages, j, np);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], fmaxf(fmaxf(x[k][0], x[k][1]), fmaxf(x[k][2], x[k][3])));
+      for (int k = 0; k < kHeads; ++k) m[k] = fmaxf(m[k], fmaxf(fmaxf(x[k][0], x[k][1]), fmaxf(x[k][2], x[k][3])));
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < kHeads; ++k) {
       m[k] = wave_max(m[k]);
       if (lane == 0) part[k][w] = m[k];
     }
     __syncthreads();
-    if (threadIdx.x < 4 && h0 + (int)threadIdx.x < A.G) {
-      float t = part[threadIdx.x][0];
-#pragma unroll
-      for (int i = 1; i < kWaves; ++i) t = fmaxf(t, part[threadIdx.x][i]);
-      top[h0 + threadIdx.x] = t;
+    if (threadIdx.x < kHeads * 16) {  // 16 lanes a head
+      float t = row16_max((int)(threadIdx.x & 15) < kWaves ? part[threadIdx.x >> 4][threadIdx.x & 15] : -INFINITY);
+      if ((threadIdx.x & 15) == 0) top[h0 + (threadIdx.x >> 4)] = t;
     }
     __syncthreads();
   }
+  const bool kept_in_registers = A.G <= kHeads && np <= 4 * T;
   for (int j = threadIdx.x; j < np; j += 4 * T) {
     float s[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 4
-    for (int h = 0; h < A.G; ++h) {
-      float x[4];
-      load4<T>(x, score + (size_t)h * A.max_pages, j, np);
+    for (int h0 = 0; h0 < A.G; h0 += kHeads) {
+      if (!kept_in_registers) load_scores<T, kHeads>(x, A, score, h0, j, np);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = vmax(s[i], x[i] - top[h]);
+      for (int k = 0; k < kHeads; ++k) {
+        const float t = top[min(h0 + k, A.G - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = vmax(s[i], x[k][i] - t);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -94,6 +107,8 @@ __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
     }
   }
 
+  __syncthreads();
+
   // The K-th largest key by its digits of 11, 11 and 10 bits; it ends early where a digit's pages are all kept.
   uint32_t prefix = 0, mask = 0, want = (uint32_t)K;
   bool whole = false;
@@ -101,17 +116,17 @@ __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
   for (int pass = 0; pass < 3 && !whole; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digits = pass == 2 ? 1023u : 2047u;
-    for (int i = threadIdx.x; i < kBins; i += T) hist[i] = 0;
-    __syncthreads();
     for (int j = threadIdx.x; j < np; j += T) {
       const uint32_t k = keys[j];
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
+      if ((k & mask) == prefix) atomicAdd(&hist[pass][(k >> shift) & digits], 1u);
     }
     __syncthreads();
+    if (pass < 2)
+      for (int i = threadIdx.x; i < kBins; i += T) hist[pass + 1][i] = 0;
     // Thread t counts bins from the largest digit down: kBins - 1 - t kPer, ...
     uint32_t c[kPer], s = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) s += c[i] = hist[kBins - 1 - (int)threadIdx.x * kPer - i];
+    for (int i = 0; i < kPer; ++i) s += c[i] = hist[pass][kBins - 1 - (int)threadIdx.x * kPer - i];
     const uint32_t incl = wave_incl_scan(s, lane);
     if (lane == 63) waves[w] = incl;
     __syncthreads();
@@ -172,31 +187,34 @@ __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
   }
 }
 
-template <int T>
+template <int T, int kHeads>
 hipError_t launch_t(const PageSelectArgs& a, hipStream_t stream) {
   static std::mutex mu;
   static bool granted[64] = {};
-  const size_t lds = ((size_t)(a.max_pages + 3) / 4 * 4 + a.G) * 4;
+  const size_t lds = ((size_t)(a.max_pages + 3) / 4 * 4 + (a.G + kHeads - 1) / kHeads * kHeads) * 4;
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  if (lds > 48 * 1024) {
+  if (lds > 32 * 1024) {
     std::lock_guard<std::mutex> lock(mu);
     if (dev < 0 || dev >= 64 || !granted[dev]) {
-      e = hipFuncSetAttribute(reinterpret_cast<const void*>(&page_select_kernel<T>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, (kMaxSelectPages + 4096) * 4);
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(&page_select_kernel<T, kHeads>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, (kMaxSelectPages + kMaxSelectHeads) * 4);
       if (e != hipSuccess) return e;
       if (dev >= 0 && dev < 64) granted[dev] = true;
     }
   }
-  hipLaunchKernelGGL((page_select_kernel<T>), dim3(a.B * a.Hkv), dim3(T), lds, stream, a);
+  hipLaunchKernelGGL((page_select_kernel<T, kHeads>), dim3(a.B * a.Hkv), dim3(T), lds, stream, a);
   return hipGetLastError();
 }
+
+static_assert((kMaxSelectPages + kMaxSelectHeads) * 4 + 3 * kBins * 4 + 1024 <= 160 * 1024, "LDS of page_select_kernel");
 
 }  // namespace
 
 hipError_t launch_page_select(const PageSelectArgs& a, hipStream_t stream) {
-  return a.max_pages <= 1024 ? launch_t<256>(a, stream) : launch_t<1024>(a, stream);
+  if (a.G <= 4) return a.max_pages <= 1024 ? launch_t<256, 4>(a, stream) : launch_t<1024, 4>(a, stream);
+  return a.max_pages <= 1024 ? launch_t<256, 8>(a, stream) : launch_t<1024, 8>(a, stream);
 }
 
 }  // namespace cosa

@@ -116,7 +116,7 @@ def test_list_and_budget_refusals():
         refused(B.COSA_ERR_INVALID_ARG, select, **kw)
     refused(B.COSA_ERR_UNSUPPORTED, select, p=change(max_pages=32769))
     refused(B.COSA_ERR_UNSUPPORTED, CALLS["sparse"], p=change(max_pages=32769))
-    refused(B.COSA_ERR_UNSUPPORTED, select, p=change(n_q_heads=2 * 4097))
+    refused(B.COSA_ERR_UNSUPPORTED, select, p=change(n_q_heads=2 * 1025))
     refused(B.COSA_ERR_INVALID_ARG, CALLS["sparse"], bounds=None)
     refused(B.COSA_ERR_INVALID_ARG, CALLS["score"], bounds=24)
 
