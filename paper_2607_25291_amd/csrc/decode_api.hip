@@ -139,6 +139,14 @@ cosa_status check_tokens(const DecodeShape& sh, int64_t pages) {
   return ok();
 }
 
+cosa_status check_score_space(const DecodeShape& sh) {
+  const int64_t waves = (int64_t)sh.B * sh.Hkv * ((sh.G + 15) / 16) *
+                        ((sh.max_pages + cosa::kScorePages - 1) / cosa::kScorePages);
+  if (waves >= (1ll << 26))  // 2^32 threads of a grid
+    return fail(COSA_ERR_UNSUPPORTED, "%d sequences of %d pages: too large for one launch", sh.B, sh.max_pages);
+  return ok();
+}
+
 cosa_status check_workspace(const void* ws, size_t bytes, size_t need) {
   if (!ws || bytes < need) return fail(COSA_ERR_WORKSPACE, "workspace of %zu bytes at %p, need %zu", bytes, ws, need);
   if (misaligned(ws, 16)) return fail(COSA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -245,8 +253,8 @@ cosa_status cosa_kv_append(int32_t n_kv_heads, int32_t head_dim, int32_t page_si
     if ((s != 0 && s < dense) || s % 8 != 0)
       return fail(COSA_ERR_INVALID_ARG, "row stride %lld: 0, or a multiple of 8 of at least n_kv_heads * head_dim = %lld",
                   (long long)s, (long long)dense);
-  if (n_tokens > (1ll << 31) / n_kv_heads) return fail(COSA_ERR_UNSUPPORTED, "%lld tokens of %d heads: too large for one launch",
-                                                      (long long)n_tokens, n_kv_heads);
+  if (n_tokens > (1ll << 29) / n_kv_heads)  // 2^32 threads of a grid, 64 for 16 rows of a head
+    return fail(COSA_ERR_UNSUPPORTED, "%lld tokens of %d heads: too large for one launch", (long long)n_tokens, n_kv_heads);
   if (n_tokens == 0) return ok();
   if (!k_cache || !v_cache || !k || !v || !slots)
     return fail(COSA_ERR_INVALID_ARG, "k_cache, v_cache, k, v and slots must be non-NULL");
@@ -274,7 +282,7 @@ cosa_status cosa_page_score(const cosa_decode_problem* problem, const void* q, c
   cosa_status st = check_problem(problem, kv->page_size, sh, empty);
   if (st != COSA_OK) return st;
   if ((st = check_kv(kv, false, sh)) != COSA_OK) return st;
-  if ((st = check_tokens(sh, sh.max_pages)) != COSA_OK) return st;
+  if ((st = check_score_space(sh)) != COSA_OK) return st;
   if (empty || sh.max_pages == 0) return ok();
   if ((st = check_q(q)) != COSA_OK) return st;
   if (!bounds || !seq_lens || !score) return fail(COSA_ERR_INVALID_ARG, "bounds, seq_lens and score must be non-NULL");
@@ -366,7 +374,7 @@ cosa_status cosa_decode_sparse(const cosa_decode_problem* problem, const void* q
   cosa_decode_sparse_layout l;
   if ((st = sparse_layout(problem, budget, any, micro, empty, l)) != COSA_OK) return st;
   if ((st = check_tokens(sh, budget->max_pages)) != COSA_OK) return st;
-  if ((st = check_tokens(sh, sh.max_pages)) != COSA_OK) return st;
+  if ((st = check_score_space(sh)) != COSA_OK) return st;
   if (empty) return ok();
   if ((st = check_q(q)) != COSA_OK) return st;
   if (!bounds || misaligned(bounds, 16)) return fail(COSA_ERR_INVALID_ARG, "bounds must be non-NULL and 16-byte aligned");

@@ -470,7 +470,8 @@ size_t decode_workspace_bytes(const DecodeShape& sh) {
 
 bool decode_fits(const DecodeShape& sh, long long tokens) {
   const long long QG = (sh.G + kRows - 1) / kRows, tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1);
-  return (long long)sh.B * sh.Hkv * QG < (1ll << 24) && (long long)sh.B * sh.Hkv * QG * tiles < (1ll << 31);
+  // 2^32 threads of a grid, in workgroups of up to 1024; tiles in 31 bits
+  return (long long)sh.B * sh.Hkv * QG < (1ll << 22) && (long long)sh.B * sh.Hkv * QG * tiles < (1ll << 31);
 }
 
 hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream) {

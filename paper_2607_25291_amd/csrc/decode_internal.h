@@ -40,6 +40,7 @@ struct AppendArgs {
 };
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream);
 
+constexpr int kScorePages = 16;  // pages of a wave of cosa_page_score
 hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uint16_t* bounds,
                              const int32_t* table, const int32_t* seq_lens, float* score,
                              hipStream_t stream);
@@ -65,7 +66,7 @@ struct DecodeArgs {
 };
 // Scratch of a decode attention call. 0: too large for one launch.
 size_t decode_workspace_bytes(const DecodeShape& sh);
-// Whether the tiles of a call (capacity `tokens` per sequence and KV head) can be numbered in 31 bits.
+// Whether the units and tiles of a call (capacity `tokens` per sequence and KV head) fit a grid and 31 bits.
 bool decode_fits(const DecodeShape& sh, long long tokens);
 hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream);
 

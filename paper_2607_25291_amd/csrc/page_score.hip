@@ -29,7 +29,7 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
   const int id = blockIdx.x;
   const int hq = id % (P.Hkv * P.QG), g = hq / P.QG, qg = hq % P.QG;
   const int ns = id / (P.Hkv * P.QG), n = ns / P.segs;
-  const int j0 = (ns % P.segs) * 16;
+  const int j0 = (ns % P.segs) * kScorePages;
   const int32_t* row = P.table + (size_t)n * P.max_pages;
   long long p = j0 + r < P.max_pages ? row[j0 + r] : 0;
   const int page = 1 << P.log2_page;
@@ -82,7 +82,7 @@ hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uin
                              const int32_t* table, const int32_t* seq_lens, float* score,
                              hipStream_t stream) {
   const int QG = (sh.G + 15) / 16;
-  const int segs = (sh.max_pages + 15) / 16, n_waves = sh.B * segs * sh.Hkv * QG;
+  const int segs = (sh.max_pages + kScorePages - 1) / kScorePages, n_waves = sh.B * segs * sh.Hkv * QG;
   const ScoreParams P{q, bounds, table, seq_lens, score, sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages,
                       sh.log2_page, segs, sh.q_stride, sh.n_pages, sh.scale,
                       sh.max_pages % 4 == 0 && reinterpret_cast<uintptr_t>(score) % 16 == 0};
