@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a paged KV cache, for gfx950: split over the tokens and
 // joined.
 //
-// A unit is (sequence, KV head, up to 16 query heads of its group). 32 keys at a time, a wave computes
+// A unit is (sequence, KV head, up to 16 or 32 query heads of its group). 32 keys at a time, a wave computes
 // S^T = K Q^T and O^T += V^T P^T with 16x16x32 MFMAs, the query heads as columns. K operands come straight
 // from the cache (lane: key l % 16, 16 bytes of its row). V operands too: lane (r, gq) reads the 16 bytes at
 // columns 8 r .. 8 r + 7 of eight keys, an 8 x 8 square that 32 byte permutes turn into eight operands
@@ -24,15 +24,26 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kTile = 32 * kWaves;  // tokens of a tile: 32 per wave
-constexpr int kGrid = 512;     // workgroups that share the tiles: two per CU
 
-constexpr int kRows = 16;      // query heads of a unit
-constexpr int kPartStride = kRows * (kHeadDim + 2);  // floats of a partial result
+// A unit takes up to 16 NQ query heads of a group: NQ 1, or 2 where a group has more than 16, so that its keys and
+// values are read once for all of them. Two take twice the accumulators, and one workgroup a CU instead of
+// two, so they pay where every workgroup has work: 32 heads per KV head, 64 / 512 / 1024 / 2048 tiles 20.8 / 25.5 /
+// 30.2 / 39.3 us (two units of 16 columns 17.1 / 24.3 / 31.3 / 42.9); 64 sequences of up to 64K, 8 KV heads 965
+// (1808).
+template <int NQ>
+constexpr int kGrid = 512 / NQ;   // workgroups that share the tiles: as many as the CUs hold
+template <int NQ>
+constexpr int kRows = 16 * NQ;    // query heads of a unit
+template <int NQ>
+constexpr int kPartStride = kRows<NQ> * (kHeadDim + 2);  // floats of a partial result
+static_assert(kGrid<1> * kPartStride<1> == kGrid<2> * kPartStride<2>, "one size of workspace");
+
+inline int groups(int G, int nq) { return (G + 16 * nq - 1) / (16 * nq); }
 
 struct DecodeParams {
   const uint16_t *q, *kc, *vc;
   const int32_t *table, *seq_lens, *pages, *count;
-  float* part;    // [2 * grid][kPartStride]: the partial results of a workgroup's first and last unit
+  float* part;    // [2 * grid][kPartStride<NQ>]: the partial results of a workgroup's first and last unit
   int2* rec;      // [units]: first and last workgroup of a unit that several share; first < 0: one had it all
   uint16_t* o;
   float* lse;
@@ -80,24 +91,29 @@ struct Tile {
 };
 
 // One unit's tiles [t0, t1) by the workgroup; the result goes to o and lse (part == nullptr) or to part.
-template <bool LISTED>
+template <bool LISTED, int NQ>
 __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg, int tokens, int t0, int t1, float* part,
-                     float (*so)[kRows][kHeadDim + 4], float (*sm)[kRows], float (*sl)[kRows]) {
+                     float (*so)[kRows<NQ>][kHeadDim + 4], float (*sm)[kRows<NQ>], float (*sl)[kRows<NQ>]) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gq = lane >> 4;
-  const int rows = min(P.G - qg * kRows, kRows);
-  const int h0 = g * P.G + qg * kRows;
+  const int rows = min(P.G - qg * kRows<NQ>, kRows<NQ>);
+  const int h0 = g * P.G + qg * kRows<NQ>;
   const int page = 1 << P.log2_page;
   const int len = seq_len(P, n);
 
-  u32x4_t qf[4];
-  const uint16_t* q = P.q + (size_t)n * P.q_stride + (size_t)(h0 + min(r, rows - 1)) * kHeadDim + gq * 8;
+  u32x4_t qf[NQ][4];
+  f32x4_t acc[NQ][8];
+  float m[NQ], l[NQ];  // running maximum (log2 units) of column r, and this lane's share of its sum
 #pragma unroll
-  for (int c = 0; c < 4; ++c) qf[c] = ldg16(q + c * 32);
-
-  f32x4_t acc[8];
+  for (int x = 0; x < NQ; ++x) {
+    const uint16_t* q =
+        P.q + (size_t)n * P.q_stride + (size_t)(h0 + min(16 * x + r, rows - 1)) * kHeadDim + gq * 8;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;  // running maximum (log2 units) of column r, and this lane's share of its sum
+    for (int c = 0; c < 4; ++c) qf[x][c] = ldg16(q + c * 32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[x][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m[x] = -INFINITY;
+    l[x] = 0.f;
+  }
 
   const unsigned begin = (unsigned)t0 * kTile + w * 32;
   const unsigned end = min((unsigned)t1 * kTile, (unsigned)tokens);
@@ -152,47 +168,50 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
     __builtin_amdgcn_sched_barrier(0);
   };
   const auto compute = [&](Tile& T, int v0, int v1) __attribute__((always_inline)) {
-    f32x4_t s[2];
+    u32x4_t ph[NQ], pl[NQ];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < NQ; ++x) {
+      f32x4_t s[2];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[h] = mfma16(T.k[h][c], qf[c], s[h]);
-    }
-    if (v0 < 16 || v1 < 16) {  // keys behind the sequence (read as zeros, as their values are): no weight
+      for (int h = 0; h < 2; ++h) {
+        s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int c = 0; c < 4; ++c) s[h] = mfma16(T.k[h][c], qf[x][c], s[h]);
+      }
+      if (v0 < 16 || v1 < 16) {  // keys behind the sequence (read as zeros, as their values are): no weight
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (gq * 4 + i >= (h ? v1 : v0)) s[h][i] = -INFINITY;
-    }
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    mx = half_max(xmax16(mx)) * P.scale_log2;
-    const float mn = fmaxf(m, mx);
-    const float base = mn == -INFINITY ? 0.f : mn;
-    const float alpha = __builtin_amdgcn_exp2f(m - base);
-    float p[8], sum = 0.f;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], P.scale_log2, -base));
-      sum += p[i];
-    }
-    l = l * alpha + sum;
-    m = mn;
-    if (__any(alpha != 1.f)) {
+          for (int i = 0; i < 4; ++i)
+            if (gq * 4 + i >= (h ? v1 : v0)) s[h][i] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                       fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+      mx = half_max(xmax16(mx)) * P.scale_log2;
+      const float mn = fmaxf(m[x], mx);
+      const float base = mn == -INFINITY ? 0.f : mn;
+      const float alpha = __builtin_amdgcn_exp2f(m[x] - base);
+      float p[8], sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], P.scale_log2, -base));
+        sum += p[i];
+      }
+      l[x] = l[x] * alpha + sum;
+      m[x] = mn;
+      if (__any(alpha != 1.f)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[e][i] *= alpha;
-    }
-    u32x4_t ph, pl;
+        for (int e = 0; e < 8; ++e)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t a, b;
-      split_bf16(p[2 * i], p[2 * i + 1], a, b);
-      ph[i] = a;
-      pl[i] = b;
+          for (int i = 0; i < 4; ++i) acc[x][e][i] *= alpha;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t a, b;
+        split_bf16(p[2 * i], p[2 * i + 1], a, b);
+        ph[x][i] = a;
+        pl[x][i] = b;
+      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -202,8 +221,11 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
       for (int i = 0; i < 4; ++i)
         a[i] = __builtin_amdgcn_perm(T.v[2 * i + 1][e >> 1], T.v[2 * i][e >> 1],
                                      (e & 1) ? 0x07060302u : 0x05040100u);
-      acc[e] = mfma16(a, ph, acc[e]);
-      acc[e] = mfma16(a, pl, acc[e]);
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        acc[x][e] = mfma16(a, ph[x], acc[x][e]);
+        acc[x][e] = mfma16(a, pl[x], acc[x][e]);
+      }
     }
   };
 
@@ -225,18 +247,22 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
   }
 
   // The waves' results: lane (r, gq) holds columns d = 8 (4 gq + i) + e of query head r.
-  l += __shfl_xor(l, 16, 64);
-  l = half_sum(l);
-  if (r < rows) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float* to = &so[w][r][8 * (4 * gq + i)];
+  for (int x = 0; x < NQ; ++x) {
+    float sum = l[x] + __shfl_xor(l[x], 16, 64);
+    sum = half_sum(sum);
+    const int row = 16 * x + r;
+    if (row < rows) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) to[e] = acc[e][i];
-    }
-    if (gq == 0) {
-      sm[w][r] = m;
-      sl[w][r] = l;
+      for (int i = 0; i < 4; ++i) {
+        float* to = &so[w][row][8 * (4 * gq + i)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[e] = acc[x][e][i];
+      }
+      if (gq == 0) {
+        sm[w][row] = m[x];
+        sl[w][row] = sum;
+      }
     }
   }
   __syncthreads();
@@ -256,8 +282,8 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
     if (part) {
       part[hh * kHeadDim + d] = O;
       if (d == 0) {
-        part[kRows * kHeadDim + hh] = M;
-        part[kRows * (kHeadDim + 1) + hh] = L;
+        part[kRows<NQ> * kHeadDim + hh] = M;
+        part[kRows<NQ> * (kHeadDim + 1) + hh] = L;
       }
     } else {
       const size_t out = (size_t)n * P.Hq + h0 + hh;
@@ -285,13 +311,13 @@ __device__ __forceinline__ int owner_of(uint32_t x, uint32_t n, uint32_t all) {
 }
 
 // WHOLE: a workgroup per unit, no splitting.
-template <bool LISTED, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
-  __shared__ float so[kWaves][kRows][kHeadDim + 4], sm[kWaves][kRows], sl[kWaves][kRows];
+template <bool LISTED, bool WHOLE, int NQ>
+__global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P) {
+  __shared__ float so[kWaves][kRows<NQ>][kHeadDim + 4], sm[kWaves][kRows<NQ>], sl[kWaves][kRows<NQ>];
   const auto unit = [&](int item, int sub, int t0, int t1, int tokens, float* part) __attribute__((always_inline)) {
     const int n = LISTED ? item / P.Hkv : item;
     const int g = LISTED ? item % P.Hkv : sub / P.QG;
-    walk<LISTED>(P, n, g, sub % P.QG, tokens, t0, t1, part, so, sm, sl);
+    walk<LISTED, NQ>(P, n, g, sub % P.QG, tokens, t0, t1, part, so, sm, sl);
   };
   if (WHOLE) {
     const int item = blockIdx.x / P.mult;
@@ -354,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(DecodeParams P) {
   for (;;) {
     const int t1 = (int)min((uint32_t)t0 + (b - a), (uint32_t)tiles);
     float* part = nullptr;
-    if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride;
+    if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride<NQ>;
     if (t0 == 0 && threadIdx.x == 0)
       P.rec[item * P.mult + sub] =
           t1 < tiles ? int2{(int)blockIdx.x, owner_of(a + tiles - 1, gridDim.x, total * P.mult)} : int2{-1, 0};
@@ -375,7 +401,7 @@ constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
 // Joins the partial results of unit blockIdx.x, for `heads` query heads from blockIdx.y * heads on. A group of 32 threads adds partial results, four columns a
 // thread; the 16 groups are dealt to the heads and, within a head, to its partial results in turn, so that
 // the loads of many wait side by side.
-template <bool LISTED>
+template <bool LISTED, int NQ>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int heads, int log2_per_head) {
   __shared__ f32x4_t sums[kJoinGroups][32];
   __shared__ float lsum[kJoinGroups], tops[kJoinGroups];
@@ -386,9 +412,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   const int t = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int per_head = 1 << log2_per_head, mine = group & (per_head - 1);
   const int slot = group >> log2_per_head, hh = blockIdx.y * heads + slot;
-  const bool live = slot < heads && qg * kRows + hh < P.G;
+  const bool live = slot < heads && qg * kRows<NQ> + hh < P.G;
   const int first = rec.x, n_parts = rec.y - first + 1;
-  const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * kPartStride; };
+  const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * kPartStride<NQ>; };
   float M = -INFINITY, L = 0.f;
   f32x4_t O = {0.f, 0.f, 0.f, 0.f};
   const auto add = [&](float m, float l, const f32x4_t& o) {
@@ -405,8 +431,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {  // behind the last part: that one again, without weight
         const float* p = part(min(i0 + i * per_head, n_parts - 1));
-        m[i] = p[kRows * kHeadDim + hh];
-        l[i] = p[kRows * (kHeadDim + 1) + hh];
+        m[i] = p[kRows<NQ> * kHeadDim + hh];
+        l[i] = p[kRows<NQ> * (kHeadDim + 1) + hh];
         o[i] = *reinterpret_cast<const f32x4_t*>(p + hh * kHeadDim + t * 4);
       }
 #pragma unroll
@@ -422,7 +448,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   __syncthreads();
   if (!live || mine != 0) return;
   for (int i = 1; i < per_head; ++i) add(tops[group + i], lsum[group + i], sums[group + i][t]);
-  const size_t out = (size_t)n * P.Hq + (size_t)g * P.G + qg * kRows + hh;
+  const size_t out = (size_t)n * P.Hq + (size_t)g * P.G + qg * kRows<NQ> + hh;
   uint16_t o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint16_t, (__bf16)(M == -INFINITY ? 0.f : O[i] / L));
@@ -431,7 +457,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   if (P.lse && t == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
 }
 
-template <bool LISTED>
+template <bool LISTED, int NQ>
 hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream) {
   const long long units = (long long)P.items * P.mult, tiles = (tokens + kTile - 1) / kTile;
   // A workgroup for every unit, and no join, where a unit is short, or less short and there are enough of them: 8
@@ -439,19 +465,19 @@ hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream)
   // 18.7 / 28.0 / 46.4 (23.5 / 32.2 / 50.0), 320 of them 24.9 / 38.3 / 71.3 (26.8 / 38.5 / 67.0), 800 of them 42.4 /
   // 80.7 / 150 (45.1 / 80.6 / 148).
   if (tokens <= 512 || (tokens <= 1024 && units >= 256)) {
-    hipLaunchKernelGGL((decode_kernel<LISTED, true>), dim3((unsigned)units), dim3(kThreads), 0, stream, P);
+    hipLaunchKernelGGL((decode_kernel<LISTED, true, NQ>), dim3((unsigned)units), dim3(kThreads), 0, stream, P);
     return hipGetLastError();
   }
-  const int grid = (int)std::min<long long>(units * tiles, kGrid);
-  hipLaunchKernelGGL((decode_kernel<LISTED, false>), dim3(grid), dim3(kThreads), 0, stream, P);
+  const int grid = (int)std::min<long long>(units * tiles, kGrid<NQ>);
+  hipLaunchKernelGGL((decode_kernel<LISTED, false, NQ>), dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // Few units leave many partial results each: then every head has workgroups of its own.
-  const int rows = std::min(P.G, kRows), parts = (int)std::min<long long>(std::max<long long>(256 / units, 1), rows);
-  const int heads = (rows + parts - 1) / parts;
+  const int rows = std::min(P.G, kRows<NQ>), parts = (int)std::min<long long>(std::max<long long>(256 / units, 1), rows);
+  const int heads = std::min((rows + parts - 1) / parts, kJoinGroups);
   int log2_per_head = 4;
   while (heads << log2_per_head > kJoinGroups) --log2_per_head;
-  hipLaunchKernelGGL((join_kernel<LISTED>), dim3((unsigned)units, (rows + heads - 1) / heads), dim3(kJoinThreads), 0, stream, P,
+  hipLaunchKernelGGL((join_kernel<LISTED, NQ>), dim3((unsigned)units, (rows + heads - 1) / heads), dim3(kJoinThreads), 0, stream, P,
                      heads, log2_per_head);
   return hipGetLastError();
 }
@@ -460,31 +486,32 @@ hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream)
 
 // The workspace: a record per unit, then two partial results per workgroup.
 static size_t record_bytes(const DecodeShape& sh) {
-  const size_t units = (size_t)sh.B * sh.Hkv * ((sh.G + kRows - 1) / kRows);
-  return (units * sizeof(int2) + 255) / 256 * 256;
+  return ((size_t)sh.B * sh.Hkv * groups(sh.G, 1) * sizeof(int2) + 255) / 256 * 256;
 }
 
 size_t decode_workspace_bytes(const DecodeShape& sh) {
-  return record_bytes(sh) + (size_t)kGrid * 2 * kPartStride * sizeof(float);
+  return record_bytes(sh) + (size_t)kGrid<1> * 2 * kPartStride<1> * sizeof(float);
 }
 
 bool decode_fits(const DecodeShape& sh, long long tokens) {
-  const long long QG = (sh.G + kRows - 1) / kRows, tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1);
+  const long long units = (long long)sh.B * sh.Hkv * groups(sh.G, 1), tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1);
   // 2^32 threads of a grid, in workgroups of up to 1024; tiles in 31 bits
-  return (long long)sh.B * sh.Hkv * QG < (1ll << 22) && (long long)sh.B * sh.Hkv * QG * tiles < (1ll << 31);
+  return units < (1ll << 22) && units * tiles < (1ll << 31);
 }
 
 hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream) {
-  const int QG = (sh.G + kRows - 1) / kRows;
+  const bool listed = a.pages != nullptr;
+  const long long tokens = listed ? (long long)a.list_pages << sh.log2_page : sh.cap();
+  const int nq = sh.G > 16 && (long long)sh.B * sh.Hkv * ((tokens + kTile - 1) / kTile) > kGrid<1> ? 2 : 1;
+  const int QG = groups(sh.G, nq);
   int2* rec = static_cast<int2*>(a.workspace);
   float* part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + record_bytes(sh));
-  const bool listed = a.pages != nullptr;
   const DecodeParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.pages, a.count, part, rec, a.o, a.lse,
                        sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages, sh.log2_page, a.list_pages,
                        listed ? sh.B * sh.Hkv : sh.B, listed ? QG : sh.Hkv * QG, sh.q_stride, sh.n_pages,
                        sh.scale * 1.4426950408889634f};
-  return listed ? launch_t<true>(P, (long long)a.list_pages << sh.log2_page, stream)
-                : launch_t<false>(P, sh.cap(), stream);
+  if (nq == 1) return listed ? launch_t<true, 1>(P, tokens, stream) : launch_t<false, 1>(P, tokens, stream);
+  return listed ? launch_t<true, 2>(P, tokens, stream) : launch_t<false, 2>(P, tokens, stream);
 }
 
 }  // namespace cosa

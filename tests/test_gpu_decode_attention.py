@@ -34,6 +34,13 @@ CASES = {
     "one_page": ([3000], 8, 1, 4096, None),
     "many_short": ([1 + 7 * i % 90 for i in range(300)], 8, 4, 16, 64),
     "long_one": ([20000], 4, 1, 128, None),
+    "gqa20": ([1300, 70, 5000], 40, 2, 32, None),
+    "gqa32": ([4100], 32, 1, 128, None),
+    "gqa24_wide": ([4100, 900, 33], 48, 2, 64, 400),   # 32 columns: more tiles than workgroups
+    "gqa70_wide": ([1500, 300], 70, 1, 32, 1100),
+    # more sequences than lanes and than threads, split (tables of more than 1024 tokens)
+    "many_mixed": ([1 + 37 * i % 2600 for i in range(90)], 4, 1, 64, None),
+    "very_many": ([1 + 13 * i % 41 for i in range(1100)], 2, 1, 16, 70),
     "batch_mixed": ([1, 6000, 40, 2500, 0, 129, 9000, 300], 8, 2, 32, None),
 }
 
@@ -54,7 +61,8 @@ def test_all_pages(name):
     assert torch().equal(o, o2)
 
 
-@pytest.mark.parametrize("name", ["tiny_mix", "gqa4", "gqa17", "batch_mixed", "many_short"])
+@pytest.mark.parametrize("name", ["tiny_mix", "gqa4", "gqa17", "gqa20", "gqa24_wide", "batch_mixed", "many_short",
+                                  "many_mixed"])
 def test_listed_pages(name):
     lens, hq, hkv, page, width = CASES[name]
     say(f"[decode listed] {name}")
@@ -101,6 +109,23 @@ def test_list_of_all_pages_matches_the_whole_walk():
     a, b = as_f64(o), as_f64(o2)
     assert (np.abs(a - b) <= 2.0 ** -7 * np.maximum(np.abs(a), np.abs(b)) + 2.0 ** -12).all()
     assert torch().equal(torch().isneginf(lse), torch().isneginf(lse2))
+
+
+def test_walks_of_many_steps():
+    """Lists long enough that a wave looks up its pages more than once: three pages, each listed 100000 times, have the
+    weights of the three pages listed once, and a sum 100000 times as large."""
+    t = torch()
+    rng = np.random.default_rng(11)
+    c = Cache(rng, [44], 1, 16, spare=1)
+    q = normal(rng, 1, 3, 128)
+    p = B.DecodeProblem(1, 3, 1, c.width)
+    pages = np.tile(np.arange(3, dtype=np.int32), (1, 1, 100000))
+    say(f"[decode steps] a list of {pages.size} pages")
+    o, lse = run_decode(p, c, dev(q), (pages, np.full((1, 1), pages.size, np.int32)))
+    ro, rl, wt, mag = D.decode_attention(q, c.k, c.v, c.table, [44])
+    check_attention(as_f64(o), lse.cpu().numpy().astype(np.float64), (ro, rl + np.log(100000.0), wt, mag),
+                    pages.size * 16)
+    assert t.isfinite(lse).all()
 
 
 def test_lengths_and_tables_outside_their_range():

@@ -95,6 +95,7 @@ def check_append(heads, page, kc, vc, bounds, k, v, slots):
 @pytest.mark.parametrize("heads,page,lens,new", [
     (1, 16, [1], [1]), (2, 16, [16, 17, 33], [1, 1, 1]), (8, 64, [64, 65, 100, 1, 128], [64, 1, 36, 1, 65]),
     (5, 32, [700, 3, 90], [650, 0, 90]), (8, 256, [1100, 255], [1001, 254]), (2, 128, [5000] * 3, [4900, 77, 1]),
+    (1, 512, [513, 1500, 30], [513, 700, 1]), (3, 2048, [4100, 2040, 2050], [3000, 1, 5]), (1, 16, [9000] * 4, [8999] * 4),
 ])
 def test_append(heads, page, lens, new, with_bounds):
     say(f"[append] heads {heads} page {page} lens {lens} new {new}")
