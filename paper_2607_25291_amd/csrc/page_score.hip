@@ -23,7 +23,7 @@ struct ScoreParams {
 // A wave scores 16 pages. Waves that follow each other take the KV heads of the same pages, so that a page's
 // bounds, contiguous over its heads, are read at about one time. Lengths, table entries and queries are loaded
 // side by side: a table entry is read before it is known to be in use.
-template <bool ONCE>
+template <bool ONCE, int NQ>
 __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
   const int lane = threadIdx.x, r = lane & 15, gq = lane >> 4;
   const int id = blockIdx.x;
@@ -36,44 +36,55 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
   const int len = min(max(P.seq_lens[n], 0), P.max_pages << P.log2_page);
   const int np = (int)(((unsigned)len + page - 1) >> P.log2_page);
   if (j0 >= np) return;
-  // Columns behind the group's heads repeat its last one; they are not stored.
-  const int h = g * P.G + min(qg * 16 + r, P.G - 1);
-  const uint16_t* q = P.q + (size_t)n * P.q_stride + (size_t)h * kHeadDim + gq * 8;
-  u32x4_t qp[4], qm[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const u32x4_t x = ldg16(q + c * 32);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t neg = ((x[i] >> 15) & 0x00010001u) * 0xffffu;  // all ones in halves with the sign set
-      qp[c][i] = x[i] & ~neg;
-      qm[c][i] = x[i] & neg;
-    }
-  }
   if (p < 0 || p >= P.n_pages) p = 0;
   const int page_of_lane = (int)p;
-  const bool stores = qg * 16 + r < P.G;
-  float* out = P.score + ((size_t)n * P.Hq + h) * P.max_pages;
+  u32x4_t qf[NQ][4];
+  const uint16_t* q = P.q + (size_t)n * P.q_stride + gq * 8;
+#pragma unroll
+  for (int y = 0; y < NQ; ++y) {
+    // Columns behind the group's heads repeat its last one; they are not stored.
+    const int h = g * P.G + min((qg * NQ + y) * 16 + r, P.G - 1);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) qf[y][c] = ldg16(q + (size_t)h * kHeadDim + c * 32);
+  }
   RowOperands<4, ONCE> x;  // minimum, then maximum
   x.load(lane, [&](int k) __attribute__((always_inline)) {
     const size_t pg = (unsigned)__shfl(page_of_lane, k, 64);
     return P.bounds + (pg * P.Hkv + g) * 2 * kHeadDim;
   });
   x.to_operands();
-  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < 4; ++c) acc = mfma16(x.x[c], qm[c], acc);
+  for (int y = 0; y < NQ; ++y) {
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < 4; ++c) acc = mfma16(x.x[4 + c], qp[c], acc);
-  if (!stores) return;
-  out += j0 + gq * 4;
-  if (P.wide && j0 + gq * 4 + 3 < np) {
-    *reinterpret_cast<f32x4_t*>(out) = acc * P.scale;
-  } else {
+    for (int c = 0; c < 4; ++c) {
+      u32x4_t qp, qm;
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
-      if (j0 + gq * 4 + v < np) out[v] = acc[v] * P.scale;
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t neg = ((qf[y][c][i] >> 15) & 0x00010001u) * 0xffffu;  // all ones in halves with the sign set
+        qp[i] = qf[y][c][i] & ~neg;
+        qm[i] = qf[y][c][i] & neg;
+      }
+      acc = mfma16(x.x[c], qm, acc);
+      acc = mfma16(x.x[4 + c], qp, acc);
+    }
+    const int hh = (qg * NQ + y) * 16 + r;
+    if (hh >= P.G) continue;
+    float* out = P.score + ((size_t)n * P.Hq + g * P.G + hh) * P.max_pages + j0 + gq * 4;
+    if (P.wide && j0 + gq * 4 + 3 < np) {
+      *reinterpret_cast<f32x4_t*>(out) = acc * P.scale;
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (j0 + gq * 4 + v < np) out[v] = acc[v] * P.scale;
+    }
   }
+}
+
+template <bool ONCE>
+void launch_t(const ScoreParams& P, int n_waves, hipStream_t stream) {
+  if (P.G > 16) hipLaunchKernelGGL((page_score_kernel<ONCE, 2>), dim3(n_waves), dim3(64), 0, stream, P);
+  else hipLaunchKernelGGL((page_score_kernel<ONCE, 1>), dim3(n_waves), dim3(64), 0, stream, P);
 }
 
 }  // namespace
@@ -81,7 +92,7 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
 hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uint16_t* bounds,
                              const int32_t* table, const int32_t* seq_lens, float* score,
                              hipStream_t stream) {
-  const int QG = (sh.G + 15) / 16;
+  const int QG = sh.G > 16 ? (sh.G + 31) / 32 : 1;  // a group's heads in 16 or 32 columns a wave
   const int segs = (sh.max_pages + kScorePages - 1) / kScorePages, n_waves = sh.B * segs * sh.Hkv * QG;
   const ScoreParams P{q, bounds, table, seq_lens, score, sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages,
                       sh.log2_page, segs, sh.q_stride, sh.n_pages, sh.scale,
@@ -89,10 +100,8 @@ hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uin
   // Bounds that fit the 256 MB of the last-level cache may still be there from the step before: plain loads keep
   // them (75 MB: 23.4 us, 25.2 with loads that do not). Larger ones only push others out (307 MB: 76.9 us
   // and 74.7).
-  if (sh.n_pages * sh.Hkv * (4 * kHeadDim) <= 256ll << 20)
-    hipLaunchKernelGGL((page_score_kernel<false>), dim3(n_waves), dim3(64), 0, stream, P);
-  else
-    hipLaunchKernelGGL((page_score_kernel<true>), dim3(n_waves), dim3(64), 0, stream, P);
+  if (sh.n_pages * sh.Hkv * (4 * kHeadDim) <= 256ll << 20) launch_t<false>(P, n_waves, stream);
+  else launch_t<true>(P, n_waves, stream);
   return hipGetLastError();
 }
 
