@@ -19,7 +19,8 @@
  *   - Lengths, tables, lists and slots are device data that the host does not see, so that a step
  *     can be captured into a graph and replayed with others. What they may hold is bounded on the
  *     device as each entry point says; nothing outside the given buffers is read or written.
- *   - Calls that may run at the same time need distinct workspaces and outputs.
+ *   - Calls that may run at the same time need distinct workspaces and outputs. Outputs must not overlap
+ *     inputs (o and q, and the arrays of cosa_page_map, are checked).
  *   - bf16 pointers (q, k, v, caches, bounds, o) and workspaces are 16-byte aligned; row strides are
  *     multiples of 8 elements.
  *

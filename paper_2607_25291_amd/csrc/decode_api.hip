@@ -52,6 +52,16 @@ cosa_status launch(void* stream, const char* what, F&& f) {
 
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
+// A range of memory that a call reads or writes.
+struct Span {
+  const void* p;
+  int64_t bytes;
+  bool meets(const Span& o) const {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && bytes > 0 && o.bytes > 0 && a < b + (uintptr_t)o.bytes && b < a + (uintptr_t)bytes;
+  }
+};
+
 cosa_status check_page_size(int ps, int& log2_page) {
   if (ps < 16 || ps > (1 << 20) || (ps & (ps - 1)) != 0)
     return fail(COSA_ERR_INVALID_ARG, "page_size %d is not a power of two in [16, 2^20]", ps);
@@ -158,6 +168,16 @@ cosa_status check_q(const void* q) {
   return ok();
 }
 
+// Other workgroups may still read queries when one writes its outputs.
+cosa_status check_o(const DecodeShape& sh, const void* q, const int32_t* seq_lens, const void* o) {
+  if (!seq_lens || !o || misaligned(o, 16))
+    return fail(COSA_ERR_INVALID_ARG, "seq_lens and o must be non-NULL, o 16-byte aligned");
+  const int64_t row = 2ll * sh.Hq * cosa::kHeadDim;
+  if (Span{q, 2 * (sh.B - 1) * sh.q_stride + row}.meets({o, sh.B * row}))
+    return fail(COSA_ERR_INVALID_ARG, "o must not overlap q");
+  return ok();
+}
+
 const uint16_t* u16(const void* p) { return static_cast<const uint16_t*>(p); }
 
 // Problem, cache and lengths of the attention calls, up to the workspace.
@@ -173,8 +193,7 @@ cosa_status attention(const DecodeShape& sh, const cosa_paged_kv* kv, const void
                       void* o, float* lse, void* stream) {
   cosa_status st = check_q(q);
   if (st != COSA_OK) return st;
-  if (!seq_lens || !o) return fail(COSA_ERR_INVALID_ARG, "seq_lens and o must be non-NULL");
-  if (misaligned(o, 16)) return fail(COSA_ERR_INVALID_ARG, "o must be 16-byte aligned");
+  if ((st = check_o(sh, q, seq_lens, o)) != COSA_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, cosa::decode_workspace_bytes(sh))) != COSA_OK) return st;
   const cosa::DecodeArgs a{u16(q), u16(kv->k_cache), u16(kv->v_cache), kv->page_table, seq_lens, pages, count,
                            list_pages, workspace, static_cast<uint16_t*>(o), lse};
@@ -221,6 +240,17 @@ cosa_status cosa_page_map(int32_t batch, int32_t page_size, int32_t max_pages, c
     return fail(COSA_ERR_INVALID_ARG, "cached_lens, new_lens, n_free, seq_lens, cu_new and n_taken must be non-NULL");
   if ((free_capacity > 0 && !free_pages) || (max_pages > 0 && !page_table) || (max_new > 0 && !slots))
     return fail(COSA_ERR_INVALID_ARG, "free_pages, page_table and slots must be non-NULL where they hold entries");
+  const int64_t n = batch;
+  const Span in[] = {{cached_lens, 4 * n}, {new_lens, 4 * n}, {free_pages, 4ll * free_capacity}, {n_free, 4}};
+  const Span out[] = {{page_table, 4 * n * max_pages}, {seq_lens, 4 * n}, {cu_new, 4 * (n + 1)}, {slots, 8ll * max_new},
+                      {n_taken, 4}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (o.meets(i))
+        return fail(COSA_ERR_INVALID_ARG, "page_table, seq_lens, cu_new, slots and n_taken must not overlap the inputs");
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (out[i].meets(out[j])) return fail(COSA_ERR_INVALID_ARG, "the outputs must not overlap each other");
   a.batch = batch;
   a.max_pages = max_pages;
   a.free_capacity = free_capacity;
@@ -378,8 +408,7 @@ cosa_status cosa_decode_sparse(const cosa_decode_problem* problem, const void* q
   if (empty) return ok();
   if ((st = check_q(q)) != COSA_OK) return st;
   if (!bounds || misaligned(bounds, 16)) return fail(COSA_ERR_INVALID_ARG, "bounds must be non-NULL and 16-byte aligned");
-  if (!seq_lens || !o || misaligned(o, 16))
-    return fail(COSA_ERR_INVALID_ARG, "seq_lens and o must be non-NULL, o 16-byte aligned");
+  if ((st = check_o(sh, q, seq_lens, o)) != COSA_OK) return st;
   if ((st = check_workspace(workspace, workspace_bytes, l.total)) != COSA_OK) return st;
   char* ws = static_cast<char*>(workspace);
   float* score = reinterpret_cast<float*>(ws + l.score);

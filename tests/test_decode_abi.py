@@ -29,11 +29,11 @@ def change(**kw):
 CALLS = {
     "score": lambda p=GOOD, c=None, q=16, bounds=16, lens=16, out=16: B.cosa_page_score(
         p, q, c or kv(), bounds, lens, out, stream=0),
-    "decode": lambda p=GOOD, c=None, q=16, lens=16, ws=256, n=WS, o=16: B.cosa_decode_attention(
+    "decode": lambda p=GOOD, c=None, q=16, lens=16, ws=256, n=WS, o=1 << 30: B.cosa_decode_attention(
         p, q, c or kv(), lens, ws, n, o, stream=0),
-    "listed": lambda p=GOOD, c=None, q=16, lens=16, ws=256, n=WS, o=16, pages=16, count=16, width=8:
+    "listed": lambda p=GOOD, c=None, q=16, lens=16, ws=256, n=WS, o=1 << 30, pages=16, count=16, width=8:
         B.cosa_decode_attention_listed(p, q, c or kv(), lens, pages, count, width, ws, n, o, stream=0),
-    "sparse": lambda p=GOOD, c=None, q=16, bounds=16, lens=16, budget=BUDGET, ws=256, n=WS, o=16:
+    "sparse": lambda p=GOOD, c=None, q=16, bounds=16, lens=16, budget=BUDGET, ws=256, n=WS, o=1 << 30:
         B.cosa_decode_sparse(p, q, c or kv(), bounds, lens, budget, ws, n, o, stream=0),
 }
 
@@ -86,6 +86,12 @@ def test_cache_refusals(call):
     refused(B.COSA_ERR_INVALID_ARG, CALLS[call], q=8)
     refused(B.COSA_ERR_INVALID_ARG, CALLS[call], lens=None)
     refused(B.COSA_ERR_INVALID_ARG, CALLS[call], **{"out" if call == "score" else "o": None})
+    if call != "score":
+        # queries of 4 sequences, 2048 bytes each: o inside them, and just behind
+        for o in (16, 16 + 4 * 2048 - 16):
+            refused(B.COSA_ERR_INVALID_ARG, CALLS[call], o=o)
+            assert "overlap" in B.cosa_last_error()
+        refused(B.COSA_ERR_WORKSPACE, CALLS[call], o=16 + 4 * 2048, ws=None)
 
 
 def test_workspace_refusals():
@@ -122,13 +128,18 @@ def test_list_and_budget_refusals():
 
 
 def test_page_map_refusals():
-    def call(batch=4, page=16, width=8, cached=16, new=16, free=16, cap=5, n_free=16, table=16, lens=16, cu=16,
-             slots=16, rows=9, taken=16):
+    def call(batch=4, page=16, width=8, cached=4096, new=8192, free=12288, cap=5, n_free=16384, table=20480, lens=24576,
+             cu=28672, slots=32768, rows=9, taken=36864):
         B.cosa_page_map(batch, page, width, cached, new, free, cap, n_free, table, lens, cu, slots, rows, taken, stream=0)
     for kw in (dict(batch=-1), dict(page=0), dict(page=20), dict(width=-1), dict(cap=-1), dict(rows=-1),
                dict(cached=None), dict(new=None), dict(free=None), dict(n_free=None), dict(table=None),
                dict(lens=None), dict(cu=None), dict(slots=None), dict(taken=None)):
         refused(B.COSA_ERR_INVALID_ARG, call, **kw)
+    # in place, one array for two outputs, the end of one in the other
+    for kw in (dict(lens=4096), dict(lens=8192), dict(taken=16384), dict(table=12288), dict(cu=24576),
+               dict(taken=32768 + 8 * 9 - 4), dict(table=24576 - 4 * 4 * 8 + 4), dict(cu=4096 - 4 * 5 + 4)):
+        refused(B.COSA_ERR_INVALID_ARG, call, **kw)
+        assert "overlap" in B.cosa_last_error()
     refused(B.COSA_ERR_UNSUPPORTED, call, batch=8193)
     refused(B.COSA_ERR_UNSUPPORTED, call, width=1 << 27)
 
