@@ -486,8 +486,10 @@ def _place(stream, *tensors):
     pointers. They must be contiguous and share one device; None and raw pointers pass through."""
     device, out = None, []
     for t in tensors:
-        if t is not None and not isinstance(t, int):
-            device = _device(t, device)
+        if t is not None and t.__class__ is not int:
+            d = t.get_device()
+            if d != device:
+                device = _same_device(d, device)
             if not t.is_contiguous():
                 raise ValueError("tensors must be contiguous")
             t = t.data_ptr()
@@ -495,13 +497,11 @@ def _place(stream, *tensors):
     return _stream_of(stream, device), out
 
 
-def _device(t, device: Optional[int]) -> int:
-    d = t.get_device()
-    if d != device:
-        if d < 0:
-            raise ValueError("tensors must live on the GPU")
-        if device is not None:
-            raise ValueError(f"tensors must live on one device, not on cuda:{device} and cuda:{d}")
+def _same_device(d: int, device: Optional[int]) -> int:
+    if d < 0:
+        raise ValueError("tensors must live on the GPU")
+    if device is not None and d != device:
+        raise ValueError(f"tensors must live on one device, not on cuda:{device} and cuda:{d}")
     return d
 
 
@@ -524,7 +524,7 @@ def _rows(t, stride: int, like=None):
     but may lie apart, on the device of the tensor `like`, or a raw pointer with the given stride."""
     if t is None or isinstance(t, int):
         return t, stride
-    _device(t, None if like is None or isinstance(like, int) else like.get_device())
+    _same_device(t.get_device(), None if like is None or isinstance(like, int) else like.get_device())
     if t.dim() != 3:
         raise ValueError("rows must be [n, heads, head_dim]")
     n, heads, dim = t.shape
