@@ -20,7 +20,7 @@
  *     can be captured into a graph and replayed with others. What they may hold is bounded on the
  *     device as each entry point says; nothing outside the given buffers is read or written.
  *   - Calls that may run at the same time need distinct workspaces and outputs. Outputs must not overlap
- *     inputs (o and q, and the arrays of cosa_page_map, are checked).
+ *     inputs (o and q, and the arrays of cosa_page_map and cosa_kv_append, are checked).
  *   - bf16 pointers (q, k, v, caches, bounds, o) and workspaces are 16-byte aligned; row strides are
  *     multiples of 8 elements.
  *
@@ -133,7 +133,7 @@ cosa_status cosa_page_select(const cosa_decode_problem* problem, int32_t page_si
  * (sm_scale * <q[n, h], k[t]>) applied to v[t]. q [batch, Hq, d] (q_stride between sequences), o
  * [batch, Hq, d] dense, bf16; lse (NULL to omit) fp32 [batch, Hq]: the natural logarithm of the softmax's sum of
  * exponentials. fp32 arithmetic; probabilities enter the product with V as two bf16 terms (16 bits). An
- * empty sequence gives o = 0 and lse = -inf. What the cache holds behind seq_lens does not matter (NaN
+ * empty sequence, or one whose logits are all -inf, gives o = 0 and lse = -inf. What the cache holds behind seq_lens does not matter (NaN
  * included). The tokens are split over a fixed grid and joined in a fixed order: results are
  * deterministic. The workspace is scratch of at least cosa_decode_workspace_bytes() bytes.
  */

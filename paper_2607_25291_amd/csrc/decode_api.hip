@@ -19,7 +19,8 @@ using cosa::ok;
 class OnDevice {
  public:
   explicit OnDevice(hipStream_t stream) {
-    if (stream == nullptr) return;
+    // the null stream and the per-thread one belong to whichever device is current
+    if (stream == nullptr || stream == hipStreamPerThread) return;
     hipDevice_t dev;
     if ((err_ = hipGetDevice(&before_)) != hipSuccess) return;
     if ((err_ = hipStreamGetDevice(stream, &dev)) != hipSuccess) return;
@@ -290,6 +291,17 @@ cosa_status cosa_kv_append(int32_t n_kv_heads, int32_t head_dim, int32_t page_si
     return fail(COSA_ERR_INVALID_ARG, "k_cache, v_cache, k, v and slots must be non-NULL");
   for (const void* p : {(const void*)k_cache, (const void*)v_cache, (const void*)bounds, k, v})
     if (misaligned(p, 16)) return fail(COSA_ERR_INVALID_ARG, "k_cache, v_cache, bounds, k and v must be 16-byte aligned");
+  if ((double)n_pages * (double)dense * page_size > 1e18)
+    return fail(COSA_ERR_UNSUPPORTED, "caches of %lld pages are too large", (long long)n_pages);
+  const int64_t cache = 2ll * n_pages * dense << a.log2_page, rows = n_tokens - 1;
+  const Span in[] = {{k, 2 * (rows * (k_stride ? k_stride : dense) + dense)},
+                     {v, 2 * (rows * (v_stride ? v_stride : dense) + dense)}, {slots, 8 * n_tokens}};
+  const Span out[] = {{k_cache, cache}, {v_cache, cache}, {bounds, 4 * n_pages * dense}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (o.meets(i)) return fail(COSA_ERR_INVALID_ARG, "k, v and slots must not overlap the caches and bounds");
+  if (out[0].meets(out[1]) || out[0].meets(out[2]) || out[1].meets(out[2]))
+    return fail(COSA_ERR_INVALID_ARG, "k_cache, v_cache and bounds must not overlap each other");
   a.Hkv = n_kv_heads;
   a.n_pages = n_pages;
   a.n_tokens = n_tokens;

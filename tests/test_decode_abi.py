@@ -145,12 +145,19 @@ def test_page_map_refusals():
 
 
 def test_append_refusals():
-    def call(heads=2, d=128, page=16, n_pages=4, kc=16, vc=16, bounds=16, n=3, k=16, v=16, slots=16, ks=0, vs=0):
+    def call(heads=2, d=128, page=16, n_pages=4, kc=1 << 20, vc=2 << 20, bounds=3 << 20, n=3, k=4 << 20, v=5 << 20,
+             slots=6 << 20, ks=0, vs=0):
         B.cosa_kv_append(heads, d, page, n_pages, kc, vc, bounds, n, k, v, slots, ks, vs, stream=0)
     for kw in (dict(heads=0), dict(d=0), dict(page=33), dict(n_pages=0), dict(n=-1), dict(kc=None), dict(vc=None),
                dict(k=None), dict(v=None), dict(slots=None), dict(kc=8), dict(vc=8), dict(bounds=8), dict(k=8),
                dict(v=8), dict(ks=248), dict(vs=260), dict(ks=-8)):
         refused(B.COSA_ERR_INVALID_ARG, call, **kw)
+    # rows taken from the caches, one cache for both, the last row's end in a cache
+    for kw in (dict(k=(1 << 20) + 1024), dict(v=2 << 20), dict(slots=(1 << 20) + 32768 - 8), dict(vc=1 << 20),
+               dict(bounds=(1 << 20) + 32768 - 16), dict(k=(2 << 20) - 2 * (2 * 512 + 256) + 16, ks=512),
+               dict(bounds=(4 << 20) - 4096 + 16)):
+        refused(B.COSA_ERR_INVALID_ARG, call, **kw)
+        assert "overlap" in B.cosa_last_error(), kw
     refused(B.COSA_ERR_UNSUPPORTED, call, d=64)
     refused(B.COSA_ERR_UNSUPPORTED, call, n=2 ** 31)
 

@@ -40,6 +40,9 @@ CASES = {
     "gqa70_wide": ([1500, 300], 70, 1, 32, 1100),
     # more sequences than lanes and than threads, split (tables of more than 1024 tokens)
     "many_mixed": ([1 + 37 * i % 2600 for i in range(90)], 4, 1, 64, None),
+    # 32 columns, units unsplit; split with more units than the join gives heads of their own
+    "many_short_wide": ([1 + 11 * i % 500 for i in range(260)], 20, 1, 16, 32),
+    "many_wide": ([1 + 29 * i % 1300 for i in range(140)], 48, 2, 64, 24),
     "very_many": ([1 + 13 * i % 41 for i in range(1100)], 2, 1, 16, 70),
     "batch_mixed": ([1, 6000, 40, 2500, 0, 129, 9000, 300], 8, 2, 32, None),
 }
@@ -62,7 +65,7 @@ def test_all_pages(name):
 
 
 @pytest.mark.parametrize("name", ["tiny_mix", "gqa4", "gqa17", "gqa20", "gqa24_wide", "batch_mixed", "many_short",
-                                  "many_mixed"])
+                                  "many_mixed", "many_short_wide", "many_wide"])
 def test_listed_pages(name):
     lens, hq, hkv, page, width = CASES[name]
     say(f"[decode listed] {name}")
