@@ -33,7 +33,8 @@
  *
  * The *_paged entry points take K and V from a paged KV cache (cosa_paged_kv) instead of the
  * contiguous [B, Hkv, L, d] tensors; everything else is unchanged, and on the same data their
- * results are bit-identical to the contiguous calls.
+ * results are bit-identical to the contiguous calls. cosa_decode.h declares what fills such a cache and
+ * attends to it with one new token per sequence.
  */
 #ifndef COSA_H_
 #define COSA_H_
