@@ -33,6 +33,9 @@ constexpr int kTile = 32 * kWaves;  // tokens of a tile: 32 per wave
 // two, so they pay where every workgroup has work: 32 heads per KV head, 64 / 512 / 1024 / 2048 tiles 20.8 / 25.5 /
 // 30.2 / 39.3 us (two units of 16 columns 17.1 / 24.3 / 31.3 / 42.9); 64 sequences of up to 64K, 8 KV heads 965
 // (1808).
+//
+// 512 workgroups for 16 columns: 1024 take 96.2 us for one sequence of 128K (93.2) and 91.3 for 48 lists (83), 72.8
+// for 128 sequences of up to 2K (76.3, and 63 with the slots below).
 template <int NQ>
 constexpr int kGrid = 512 / NQ;   // workgroups that share the tiles: as many as the CUs hold
 template <int NQ>
@@ -72,6 +75,12 @@ __device__ __forceinline__ int item_tokens(const DecodeParams& P, int i) {
 __device__ __forceinline__ int tiles_of(int tokens) {
   return max((int)(((unsigned)tokens + kTile - 1) / kTile), 1);
 }
+
+// Slots of a unit in the row of work: its tiles, and what taking it up costs beside them, about one tile's time. Without
+// that, ranges of many short units finish last: 128 sequences of up to 2000 tokens 82.3 / 71.0 us with events, 64
+// of up to 4000 78.4 / 72.6, one of 128K 93.6 / 94.4 (17 slots a workgroup instead of 16).
+constexpr int kUnitCost = 1;
+__device__ __forceinline__ int slots_of(int tokens) { return tiles_of(tokens) + kUnitCost; }
 
 // Two fp32 values as bf16 pairs: the nearest ones, and what they leave.
 __device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -334,7 +343,7 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
   int item;
   Range R;
   if (P.items <= 64) {  // one item a lane: every wave for itself
-    const uint32_t t = lane < P.items ? (uint32_t)tiles_of(item_tokens<LISTED>(P, lane)) : 0u;
+    const uint32_t t = lane < P.items ? (uint32_t)slots_of(item_tokens<LISTED>(P, lane)) : 0u;
     const uint32_t at = wave_incl_scan(t, lane) - t;
     total = __builtin_amdgcn_readlane(at + t, 63);
     R = range_of(blockIdx.x, gridDim.x, total * P.mult);
@@ -346,7 +355,7 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
     const int per = (P.items + kThreads - 1) / kThreads;
     const int i0 = min((int)threadIdx.x * per, P.items), i1 = min(i0 + per, P.items);
     uint32_t sum = 0;
-    for (int i = i0; i < i1; ++i) sum += (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+    for (int i = i0; i < i1; ++i) sum += (uint32_t)slots_of(item_tokens<LISTED>(P, i));
     const uint32_t incl = wave_incl_scan(sum, lane);
     if (lane == 63) waves[w] = incl;
     __syncthreads();
@@ -362,7 +371,7 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
     if (x >= at && x < at + sum) {
       int i = i0;
       for (;; ++i) {
-        const uint32_t t = (uint32_t)tiles_of(item_tokens<LISTED>(P, i));
+        const uint32_t t = (uint32_t)slots_of(item_tokens<LISTED>(P, i));
         if (x < at + t) break;
         at += t;
       }
@@ -378,18 +387,20 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
   if (a == b) return;
   int tokens = item_tokens<LISTED>(P, item);
   int tiles = tiles_of(tokens);
-  const uint32_t rem = a - before * P.mult;
-  int sub = (int)(rem / (uint32_t)tiles), t0 = (int)(rem % (uint32_t)tiles);
+  const uint32_t rem = a - before * P.mult, slots = (uint32_t)tiles + kUnitCost;
+  int sub = (int)(rem / slots), t0 = (int)(rem % slots);
   for (;;) {
-    const int t1 = (int)min((uint32_t)t0 + (b - a), (uint32_t)tiles);
-    float* part = nullptr;
-    if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride<NQ>;
-    if (t0 == 0 && threadIdx.x == 0)
-      P.rec[item * P.mult + sub] =
-          t1 < tiles ? int2{(int)blockIdx.x, owner_of(a + tiles - 1, gridDim.x, total * P.mult)} : int2{-1, 0};
-    unit(item, sub, t0, t1, tokens, part);
-    a += t1 - t0;
-    if (a >= b) return;
+    if (t0 < tiles) {
+      const int t1 = (int)min((uint32_t)t0 + (b - a), (uint32_t)tiles);
+      float* part = nullptr;
+      if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)blockIdx.x * 2 + (t0 == 0)) * kPartStride<NQ>;
+      if (t0 == 0 && threadIdx.x == 0)
+        P.rec[item * P.mult + sub] =
+            t1 < tiles ? int2{(int)blockIdx.x, owner_of(a + tiles - 1, gridDim.x, total * P.mult)} : int2{-1, 0};
+      unit(item, sub, t0, t1, tokens, part);
+    }
+    if (b - a <= (uint32_t)(tiles + kUnitCost - t0)) return;
+    a += tiles + kUnitCost - t0;
     t0 = 0;
     if (++sub == P.mult) {
       sub = 0;
@@ -464,9 +475,9 @@ template <bool LISTED, int NQ>
 hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream) {
   const long long units = (long long)P.items * P.mult, tiles = (tokens + kTile - 1) / kTile;
   // A workgroup for every unit, and no join, where a unit is short, or less short and there are enough of them: 8
-  // units of 256 / 512 / 1000 tokens 11.6 / 13.7 / 18.0 us (split 15.0 / 15.4 / 15.5); 256 units of 512 / 1000 / 2000
-  // 18.7 / 28.0 / 46.4 (23.5 / 32.2 / 50.0), 320 of them 24.9 / 38.3 / 71.3 (26.8 / 38.5 / 67.0), 800 of them 42.4 /
-  // 80.7 / 150 (45.1 / 80.6 / 148).
+  // units of 256 / 512 / 1000 tokens 11.7 / 13.8 / 18.0 us (split 16.2 / 16.3 / 16.3); 256 units of 512 / 1000
+  // 19.3 / 28.2 (24.6 / 32.5), 320 of them 25.0 / 38.5 (28.0 / 39.6), 800 of them 42.4 / 80.8 (46.6 / 82.7); of 2000
+  // tokens 46.4 / 71.3 / 150 (50.0 / 67.0 / 148).
   if (tokens <= 512 || (tokens <= 1024 && units >= 256)) {
     hipLaunchKernelGGL((decode_kernel<LISTED, true, NQ>), dim3((unsigned)units), dim3(kThreads), 0, stream, P);
     return hipGetLastError();
@@ -497,7 +508,7 @@ size_t decode_workspace_bytes(const DecodeShape& sh) {
 }
 
 bool decode_fits(const DecodeShape& sh, long long tokens) {
-  const long long units = (long long)sh.B * sh.Hkv * groups(sh.G, 1), tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1);
+  const long long units = (long long)sh.B * sh.Hkv * groups(sh.G, 1), tiles = std::max<long long>((tokens + kTile - 1) / kTile, 1) + kUnitCost;
   // 2^32 threads of a grid, in workgroups of up to 1024; tiles in 31 bits
   return units < (1ll << 22) && units * tiles < (1ll << 31);
 }

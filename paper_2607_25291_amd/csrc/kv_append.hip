@@ -148,6 +148,8 @@ hipError_t launch_t(const AppendArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
+  // A wave for every 64 tokens of a page, up to 16: 64K rows in pages of 256 / 2048 114 / 143 us with events, 253 / 962
+  // with one wave; single rows in pages of 256 12.4 us, 11.0 with one.
   switch (a.log2_page) {
     case 4: case 5: case 6: return launch_t<1>(a, stream);
     case 7: return launch_t<2>(a, stream);

@@ -213,6 +213,8 @@ static_assert((kMaxSelectPages + kMaxSelectHeads) * 4 + 3 * kBins * 4 + 1024 <= 
 }  // namespace
 
 hipError_t launch_page_select(const PageSelectArgs& a, hipStream_t stream) {
+  // 256 threads up to 1024 pages (256 rows of 1024, 4 heads: 9.3 us with events, 10.2 with 1024 threads; of 2048: 12.4
+  // and 11.1); four heads at a time where the group has no more (9.3 us, 10.2 with eight).
   if (a.G <= 4) return a.max_pages <= 1024 ? launch_t<256, 4>(a, stream) : launch_t<1024, 4>(a, stream);
   return a.max_pages <= 1024 ? launch_t<256, 8>(a, stream) : launch_t<1024, 8>(a, stream);
 }

@@ -191,6 +191,7 @@ def select(score, lens, page, hkv, budget):
     ([131072, 70000, 3], 28, 4, 32, 4096, dict(max_pages=300, sink_pages=2, recent_pages=5)),
     ([131072], 17, 1, 16, 8192, dict(max_pages=1000, min_pages=1000, sink_pages=0, recent_pages=0)),
     ([524288, 500001], 2, 1, 16, 32768, dict(max_pages=700, fraction=0.01, sink_pages=1, recent_pages=3)),
+    ([4000, 100], 16, 2, 16, 250, dict(max_pages=40, sink_pages=1, recent_pages=2)),
     ([5000] * 30, 5, 5, 16, 400, dict(max_pages=313, sink_pages=0, recent_pages=1)),
 ])
 def test_page_select(lens, hq, hkv, page, width, budget, ties):
