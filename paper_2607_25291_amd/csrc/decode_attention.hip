@@ -77,8 +77,8 @@ __device__ __forceinline__ int tiles_of(int tokens) {
 }
 
 // Slots of a unit in the row of work: its tiles, and what taking it up costs beside them, about one tile's time. Without
-// that, ranges of many short units finish last: 128 sequences of up to 2000 tokens 82.3 / 71.0 us with events, 64
-// of up to 4000 78.4 / 72.6, one of 128K 93.6 / 94.4 (17 slots a workgroup instead of 16).
+// that, ranges of many short units finish last: 128 sequences of up to 2000 tokens 82.3 us with events (71.0 with it),
+// 64 of up to 4000 78.4 (72.6); one of 128K 93.6 (94.4: 17 slots for some workgroups instead of 16).
 constexpr int kUnitCost = 1;
 __device__ __forceinline__ int slots_of(int tokens) { return tiles_of(tokens) + kUnitCost; }
 
