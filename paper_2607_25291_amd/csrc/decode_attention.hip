@@ -299,9 +299,10 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
       }
     } else {
       const size_t out = (size_t)n * P.Hq + h0 + hh;
-      const __bf16 v = (__bf16)(M == -INFINITY ? 0.f : O / L);
+      // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
+      const __bf16 v = (__bf16)(L == 0.f ? 0.f : O / L);
       P.o[out * kHeadDim + d] = __builtin_bit_cast(uint16_t, v);
-      if (P.lse && d == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
+      if (P.lse && d == 0) P.lse[out] = L == 0.f ? -INFINITY : M * 0.6931471805599453f + logf(L);
     }
   }
   __syncthreads();  // so, sm and sl are used again
@@ -412,9 +413,9 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
 
 constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
 
-// Joins the partial results of unit blockIdx.x, for `heads` query heads from blockIdx.y * heads on. A group of 32 threads adds partial results, four columns a
-// thread; the 16 groups are dealt to the heads and, within a head, to its partial results in turn, so that
-// the loads of many wait side by side.
+// Joins the partial results of unit blockIdx.x, for `heads` query heads from blockIdx.y * heads on. A group of 32
+// threads adds partial results, four columns a thread; the 16 groups are dealt to the heads and, within a
+// head, to its partial results in turn, so that the loads of many wait side by side.
 template <bool LISTED, int NQ>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int heads, int log2_per_head) {
   __shared__ f32x4_t sums[kJoinGroups][32];
@@ -465,10 +466,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   const size_t out = (size_t)n * P.Hq + (size_t)g * P.G + qg * kRows<NQ> + hh;
   uint16_t o[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint16_t, (__bf16)(M == -INFINITY ? 0.f : O[i] / L));
+  for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint16_t, (__bf16)(L == 0.f ? 0.f : O[i] / L));
   *reinterpret_cast<u32x2_t*>(P.o + out * kHeadDim + t * 4) =
       u32x2_t{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
-  if (P.lse && t == 0) P.lse[out] = M == -INFINITY ? -INFINITY : M * 0.6931471805599453f + logf(L);
+  if (P.lse && t == 0) P.lse[out] = L == 0.f ? -INFINITY : M * 0.6931471805599453f + logf(L);
 }
 
 template <bool LISTED, int NQ>

@@ -192,6 +192,24 @@ def test_infinite_and_nan_values_stay_where_they_are():
     assert t.isfinite(lse).all()
 
 
+@pytest.mark.parametrize("width", [8, 200])  # unsplit, and split over workgroups
+def test_nan_logits_are_not_hidden(width):
+    """A sequence whose only logits are NaN gives NaN, not the zeros of an empty one; a NaN query its own head."""
+    rng = np.random.default_rng(12)
+    c = Cache(rng, [1, 0, 700 if width > 8 else 100], 2, 16, width)
+    q = normal(rng, 3, 4, 128)
+    c.k[c.table[0, 0], 0, 0, 7] = 0x7FC0          # heads 0 and 1 of sequence 0
+    q[2, 3, 100] = 0xFFC0                         # head 3 of sequence 2
+    p = B.DecodeProblem(3, 4, 2, c.width)
+    o, lse = run_decode(p, c, dev(q))
+    nan = np.isnan(as_f64(o))
+    want = np.zeros_like(nan)
+    want[0, :2] = want[2, 3] = True
+    assert (nan == want).all()
+    assert (np.isnan(lse.cpu().numpy()) == want[..., 0]).all()
+    assert (as_f64(o)[1] == 0).all() and np.isneginf(lse.cpu().numpy()[1]).all()
+
+
 def test_offsets_beyond_32_bits():
     """A cache of more than 2^32 bytes per tensor, the used pages at its far end."""
     t = torch()
@@ -252,6 +270,19 @@ def test_two_streams_and_a_replayed_graph():
         t.cuda.synchronize()
         assert t.equal(o, want[turn % 3])
         assert t.equal(run_decode(p, c, qs[(turn + 1) % 3], kv=kv)[0], want[(turn + 1) % 3])
+    # a second graph of the same workspace, the two replayed in turn
+    o2 = t.zeros_like(o)
+    graph2 = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph2):
+        B.cosa_decode_attention(p, qs[2], kv, c.lens_d, ws[0], n, o2)
+    q.copy_(qs[0])
+    for _ in range(3):
+        o.zero_()
+        o2.zero_()
+        graph2.replay()
+        graph.replay()
+        t.cuda.synchronize()
+        assert t.equal(o, want[0]) and t.equal(o2, want[2])
     # other lengths, same graph
     c.lens_d.copy_(dev(np.array([0, 64, 1500], np.int32)))
     short = run_decode(p, c, qs[1], kv=B.paged_kv(c.k_d, c.v_d, c.table_d, 32, c.n_pages))[0]
