@@ -132,7 +132,7 @@ cosa_status cosa_page_select(const cosa_decode_problem* problem, int32_t page_si
  * Attention of one token per sequence: o[n, h] = softmax over the tokens t < seq_lens[n] of
  * (sm_scale * <q[n, h], k[t]>) applied to v[t]. q [batch, Hq, d] (q_stride between sequences), o
  * [batch, Hq, d] dense, bf16; lse (NULL to omit) fp32 [batch, Hq]: the natural logarithm of the softmax's sum of
- * exponentials. fp32 arithmetic; probabilities enter the product with V as two bf16 terms (16 bits). An
+ * exponentials. fp32 arithmetic; probabilities enter the product with V as three bf16 terms (all 24 bits). An
  * empty sequence, or one whose logits are all -inf, gives o = 0 and lse = -inf. What the cache holds behind seq_lens does not matter (NaN
  * included). The tokens are split over a fixed grid and joined in a fixed order: results are
  * deterministic. The workspace is scratch of at least cosa_decode_workspace_bytes() bytes.

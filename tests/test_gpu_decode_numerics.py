@@ -1,0 +1,74 @@
+"""What the attention of one new token keeps of its weights: all 32 bits of them in the product with V."""
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import decode_oracle as D
+from paper_2607_25291_amd import binding as B
+from paper_2607_25291_amd.inputs import f32_to_bf16_bits
+from tests.decode_util import Cache, as_f64, run_decode
+from tests.gpu_util import dev
+
+pytestmark = pytest.mark.gpu
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def few_elements(rng, lens, hq, hkv, page, width):
+    """A cache and queries whose logits are exact in fp32: queries of 1 and of a random number in [1, 2) in their first
+    two elements, keys with those two elements only (0 here), values of 0."""
+    c = Cache(rng, lens, hkv, page, width, sinks=False)
+    q = np.zeros((len(lens), hq, 128), np.uint16)
+    q[:, :, 0] = 0x3F80
+    q[:, :, 1] = f32_to_bf16_bits(rng.uniform(1.0, 1.99, (len(lens), hq)).astype(np.float32))
+    for x in (c.k, c.v):
+        x[x != 0x7FC0] = 0
+    return c, q
+
+
+# lengths, heads, KV heads, page, table width: one workgroup a unit, split units, 32 columns a unit
+SHAPES = {"whole": ([3, 33, 150], 4, 2, 16, 20), "split": ([3, 900, 2100], 4, 2, 16, 200),
+          "columns_32": ([3 + 11 * i % 500 for i in range(260)], 20, 1, 16, 32), "columns_32_split": ([3, 4100, 900], 48, 2, 64, 400)}
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_weights_keep_32_bits(name, listed):
+    """Tokens 1 and 2 of every sequence have logits -x and -x - 2^-12 q1 and values of opposite signs, token 0 a
+    logit of 0 and the others -3, and no values: what is left is 2^-12 of a weight, where rounding both weights to
+    16 bits leaves up to 2^-17.
+
+    The logits are exact in fp32 (20 bits). A weight is exp2 of one fused product: the rounding of scale * log2(e),
+    2^-24 of at most 3, is one factor of nearly equal size for both; its own is half a unit in the last place of a number
+    below 4 (2^-23); exp2 has one unit (2^-23). So 2^-22 for each weight of the two, and fp32 sums of their products and
+    the joins' powers of two with 2^-23 each time the two are scaled apart, which they are not in one tile: 2^-20 of
+    their sum has room for all. The sum of all weights and the joins' common factors err relative to the result
+    (longest / 128 + 548 terms of 2^-24: 2^-14), and the output is rounded to bf16: 2^-8 of itself."""
+    lens, hq, hkv, page, width = SHAPES[name]
+    say(f"[decode weights] {name} listed {listed}")
+    rng = np.random.default_rng(len(name))
+    c, q = few_elements(rng, lens, hq, hkv, page, width)
+    for n, length in enumerate(lens):
+        for j in range(-(-length // page)):
+            c.k[c.table[n, j], :, :min(page, length - j * page), 0] = 0xC040  # -3
+        at = c.table[n, 0]
+        x = f32_to_bf16_bits(-rng.uniform(0.1, 1.9, hkv).astype(np.float32))
+        c.k[at, :, 0, 0], c.k[at, :, 1, 0], c.k[at, :, 2, 0] = 0, x, x
+        c.k[at, :, 2, 1] = 0xB980  # -2^-12
+        v = f32_to_bf16_bits(rng.uniform(0.5, 2.0, (hkv, 128)).astype(np.float32))
+        c.v[at, :, 1], c.v[at, :, 2] = v, v ^ 0x8000
+    p = B.DecodeProblem(len(lens), hq, hkv, c.width, sm_scale=1.0)
+    lists = None
+    if listed:
+        pages = np.tile(np.arange(c.width, dtype=np.int32), (len(lens), hkv, 1))
+        lists = (pages, np.array([[-(-n // page)] * hkv for n in lens], np.int32))
+    o, _ = run_decode(p, c, dev(q), lists, lse=False)
+    ro, _, wt, _ = D.decode_attention(q, c.k, c.v, c.table, lens, sm_scale=1.0)
+    assert (np.abs(ro) < 2.0 ** -11 * wt).all() and (ro != 0).all()
+    err = np.abs(as_f64(o) - ro)
+    tol = (2.0 ** -8 + 2.0 ** -14) * np.abs(ro) + 2.0 ** -20 * wt
+    assert (err <= tol).all(), f"off by {err.max()}, worst ratio {(err / tol).max()}"
