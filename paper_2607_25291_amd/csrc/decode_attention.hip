@@ -20,6 +20,7 @@
 // without); keys not (no gain, and 10 % slower where a short context stays in the last-level cache).
 #include "decode_device.h"
 #include "decode_internal.h"
+#include "decode_split.h"
 #include "select_wave.h"
 
 namespace cosa {
@@ -112,7 +113,7 @@ template <bool LISTED, int NQ>
 __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg, int tokens, int t0, int t1, float* part,
                      float (*so)[kRows<NQ>][kHeadDim + 4], float (*sm)[kRows<NQ>], float (*sl)[kRows<NQ>]) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, gq = lane >> 4;
-  const int rows = min(P.G - qg * kRows<NQ>, kRows<NQ>);
+  const int rows = unit_heads(P.G, kRows<NQ>, qg);
   const int h0 = g * P.G + qg * kRows<NQ>;
   const int page = 1 << P.log2_page;
   const int len = seq_len(P, n);
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(kThreads, 2 / NQ) void decode_kernel(DecodeParams P
   }
 }
 
-constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
+constexpr int kJoinThreads = 32 * kJoinGroups;
 
 // Joins the partial results of unit blockIdx.x, for `heads` query heads from blockIdx.y * heads on. A group of 32
 // threads adds partial results, four columns a thread; the 16 groups are dealt to the heads and, within a
@@ -430,8 +431,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   const int n = LISTED ? item / P.Hkv : item, g = LISTED ? item % P.Hkv : sub / P.QG, qg = sub % P.QG;
   const int t = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int per_head = 1 << log2_per_head, mine = group & (per_head - 1);
-  const int slot = group >> log2_per_head, hh = blockIdx.y * heads + slot;
-  const bool live = slot < heads && qg * kRows<NQ> + hh < P.G;
+  const int hh = join_head(heads, log2_per_head, unit_heads(P.G, kRows<NQ>, qg), blockIdx.y, group);
+  const bool live = hh >= 0;
   const int first = rec.x, n_parts = rec.y - first + 1;
   const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * kPartStride<NQ>; };
   float M = -INFINITY, L = 0.f;
@@ -491,13 +492,9 @@ hipError_t launch_t(const DecodeParams& P, long long tokens, hipStream_t stream)
   hipLaunchKernelGGL((decode_kernel<LISTED, false, NQ>), dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // Few units leave many partial results each: then every head has workgroups of its own.
-  const int rows = std::min(P.G, kRows<NQ>), parts = (int)std::min<long long>(std::max<long long>(256 / units, 1), rows);
-  const int heads = std::min((rows + parts - 1) / parts, kJoinGroups);
-  int log2_per_head = 4;
-  while (heads << log2_per_head > kJoinGroups) --log2_per_head;
-  hipLaunchKernelGGL((join_kernel<LISTED, NQ>), dim3((unsigned)units, (rows + heads - 1) / heads), dim3(kJoinThreads), 0, stream, P,
-                     heads, log2_per_head);
+  const JoinShape j = join_shape(units, P.G, kRows<NQ>);
+  hipLaunchKernelGGL((join_kernel<LISTED, NQ>), dim3((unsigned)units, j.groups), dim3(kJoinThreads), 0, stream, P, j.heads,
+                     j.log2_per_head);
   return hipGetLastError();
 }
 
