@@ -133,8 +133,9 @@ cosa_status cosa_page_select(const cosa_decode_problem* problem, int32_t page_si
  * (sm_scale * <q[n, h], k[t]>) applied to v[t]. q [batch, Hq, d] (q_stride between sequences), o
  * [batch, Hq, d] dense, bf16; lse (NULL to omit) fp32 [batch, Hq]: the natural logarithm of the softmax's sum of
  * exponentials. fp32 arithmetic; probabilities enter the product with V as three bf16 terms (all 24 bits). An
- * empty sequence, or one whose logits are all -inf, gives o = 0 and lse = -inf. What the cache holds behind seq_lens does not matter (NaN
- * included). The tokens are split over a fixed grid and joined in a fixed order: results are
+ * empty sequence, or one whose logits are all -inf, gives o = 0 and lse = -inf. An infinite v[t] gives that infinity in its
+ * element (NaN beside one of the other sign, or where its weight is 0 or below 2^-100 of the largest); NaN values and
+ * logits give NaN. What the cache holds behind seq_lens does not matter (NaN included). The tokens are split over a fixed grid and joined in a fixed order: results are
  * deterministic. The workspace is scratch of at least cosa_decode_workspace_bytes() bytes.
  */
 size_t cosa_decode_workspace_bytes(const cosa_decode_problem* problem);

@@ -83,18 +83,23 @@ __device__ __forceinline__ int tiles_of(int tokens) {
 constexpr int kUnitCost = 1;
 __device__ __forceinline__ int slots_of(int tokens) { return tiles_of(tokens) + kUnitCost; }
 
-// Two fp32 weights as pairs of bf16 terms, three each, that together have all their bits: the nearest ones, the
-// nearest to what they leave, and the rest (8 bits each). Two terms leave up to 2^-18 of a weight; the third one's
-// products are free under the memory bound (two / three, events: 128K 94.5 to 98.0 / 97.4 to 98.0 us, 64 sequences of up to 64K
-// 613 to 637 / 638 to 639, with 32 heads per KV head 952 to 962 / 953 to 960).
+// Two fp32 weights as pairs of bf16 terms, three each, that together have all their bits. Two terms leave up to 2^-18 of a
+// weight; the third one's products are free under the memory bound (two / three, events: 128K 98.0 / 97.4 to 98.2 us, 64
+// sequences of up to 64K 637 / 637 to 639, with 32 heads per KV head 952 to 962 / 953 to 976).
+// Every term of a weight that is not 0 is above 0, so that an infinite value gives infinity in each product and not
+// NaN: the first one is the largest bf16 value below the weight (at most 17 bits are left, 16 if not a power of two), the
+// second one the largest below what is left, and then 8 bits are left. (Weights below 2^-110 lose terms.)
 __device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&term)[3]) {
-  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-  typedef float f32x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int t = 0; t < 3; ++t) {
-    term[t] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
-    a -= __uint_as_float(term[t] << 16);
-    b -= __uint_as_float(term[t] & 0xffff0000u);
+    uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    if (t < 2) {
+      x = __builtin_elementwise_sub_sat(x, 1u) & 0xffff0000u;  // 0 stays 0
+      y = __builtin_elementwise_sub_sat(y, 1u) & 0xffff0000u;
+      a -= __uint_as_float(x);
+      b -= __uint_as_float(y);
+    }
+    term[t] = __builtin_amdgcn_perm(y, x, 0x07060302u);
   }
 }
 

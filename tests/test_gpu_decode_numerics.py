@@ -1,4 +1,5 @@
-"""What the attention of one new token keeps of its weights: all 32 bits of them in the product with V."""
+"""What the attention of one new token keeps of its weights and values: all 32 bits of a weight in the product with V,
+and infinite values."""
 import sys
 
 import numpy as np
@@ -7,7 +8,7 @@ import pytest
 from oracle import decode_oracle as D
 from paper_2607_25291_amd import binding as B
 from paper_2607_25291_amd.inputs import f32_to_bf16_bits
-from tests.decode_util import Cache, as_f64, run_decode
+from tests.decode_util import Cache, as_f64, check_attention, run_decode
 from tests.gpu_util import dev
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +73,40 @@ def test_weights_keep_32_bits(name, listed):
     err = np.abs(as_f64(o) - ro)
     tol = (2.0 ** -8 + 2.0 ** -14) * np.abs(ro) + 2.0 ** -20 * wt
     assert (err <= tol).all(), f"off by {err.max()}, worst ratio {(err / tol).max()}"
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_infinite_values(name, listed):
+    """An infinite value with any weight down to 2^-92 of the largest gives that infinity in its element, one of either
+    sign NaN; the other elements stay what they are. Logits of 0 to -64, one for each token (mod 65)."""
+    lens, hq, hkv, page, width = SHAPES[name]
+    say(f"[decode infinite values] {name} listed {listed}")
+    rng = np.random.default_rng(len(name) + 7)
+    c, q = few_elements(rng, lens, hq, hkv, page, width)
+    for n, length in enumerate(lens):
+        at = lambda i: (c.table[n, i // page], slice(None), i % page)
+        for i in range(length):
+            c.k[at(i)][:, 0] = f32_to_bf16_bits(np.array(-(i % 65), np.float32))
+            c.v[at(i)] = f32_to_bf16_bits(rng.standard_normal((hkv, 128)).astype(np.float32))
+        for h in range(hkv):
+            for d in range(64):  # one token in elements 0 .. 31, two in 32 .. 63, of opposite signs from 48 on
+                i, j = (int(x) for x in rng.integers(0, length, 2))
+                i, j = (i, j) if d >= 4 else (0, 0)  # elements 0 .. 3: the token of largest weight
+                sign = 0x8000 * int(rng.integers(0, 2))
+                c.v[c.table[n, i // page], h, i % page, d] = 0x7F80 | sign
+                if d >= 32 and i != j:
+                    c.v[c.table[n, j // page], h, j % page, d] = 0x7F80 | (sign if d < 48 else 0x8000 - sign)
+    p = B.DecodeProblem(len(lens), hq, hkv, c.width, sm_scale=1.0)
+    lists = None
+    if listed:
+        pages = np.tile(np.arange(c.width, dtype=np.int32), (len(lens), hkv, 1))
+        lists = (pages, np.array([[-(-n // page)] * hkv for n in lens], np.int32))
+    o, lse = run_decode(p, c, dev(q), lists)
+    with np.errstate(invalid="ignore"):
+        ro, rl, wt, mag = D.decode_attention(q, c.k, c.v, c.table, lens, sm_scale=1.0)
+    assert np.isinf(ro).any() and np.isnan(ro).any()
+    got, odd = as_f64(o), ~np.isfinite(ro)
+    assert np.array_equal(got[odd], ro[odd], equal_nan=True)
+    wt[odd] = ro[odd] = got[odd] = 0
+    check_attention(got, lse.cpu().numpy().astype(np.float64), (ro, rl, wt, mag), max(lens))
