@@ -76,7 +76,8 @@ typedef struct {
  * the first two) exceed n_free and it needs one. Such a request adds nothing: its seq_lens is cached_lens, its
  * slots are -1, it takes no page. Negative lengths are read as 0, cached lengths above the row's capacity as that
  * capacity. The old part of a row is read only for the page that is partly filled; a negative entry
- * there gives slots of -1. batch <= 8192.
+ * there gives slots of -1. batch <= 8192. An empty batch writes cu_new[0] = 0, n_taken = 0 and slots of -1, each
+ * of them unless it is NULL; its other arrays are not used.
  */
 cosa_status cosa_page_map(int32_t batch, int32_t page_size, int32_t max_pages,
                           const int32_t* cached_lens, const int32_t* new_lens,

@@ -236,13 +236,15 @@ cosa_status cosa_page_map(int32_t batch, int32_t page_size, int32_t max_pages, c
     return fail(COSA_ERR_UNSUPPORTED, "max_pages (%d) * page_size (%d) must stay below 2^31 tokens", max_pages, page_size);
   if (batch > cosa::kMaxRequests)
     return fail(COSA_ERR_UNSUPPORTED, "%d requests (supported: <= %d)", batch, cosa::kMaxRequests);
-  if (batch == 0) return ok();
-  if (!cached_lens || !new_lens || !n_free || !seq_lens || !cu_new || !n_taken)
+  const bool some = batch > 0;  // an empty batch still has rows without a request, and takes no page
+  if (some && (!cached_lens || !new_lens || !n_free || !seq_lens || !cu_new || !n_taken))
     return fail(COSA_ERR_INVALID_ARG, "cached_lens, new_lens, n_free, seq_lens, cu_new and n_taken must be non-NULL");
-  if ((free_capacity > 0 && !free_pages) || (max_pages > 0 && !page_table) || (max_new > 0 && !slots))
+  if (some && ((free_capacity > 0 && !free_pages) || (max_pages > 0 && !page_table) || (max_new > 0 && !slots)))
     return fail(COSA_ERR_INVALID_ARG, "free_pages, page_table and slots must be non-NULL where they hold entries");
+  if (!some && !cu_new && !n_taken && (max_new == 0 || !slots)) return ok();
   const int64_t n = batch;
-  const Span in[] = {{cached_lens, 4 * n}, {new_lens, 4 * n}, {free_pages, 4ll * free_capacity}, {n_free, 4}};
+  const Span in[] = {{cached_lens, 4 * n}, {new_lens, 4 * n}, {free_pages, some ? 4ll * free_capacity : 0},
+                     {n_free, some ? 4 : 0}};
   const Span out[] = {{page_table, 4 * n * max_pages}, {seq_lens, 4 * n}, {cu_new, 4 * (n + 1)}, {slots, 8ll * max_new},
                       {n_taken, 4}};
   for (const Span& o : out)
@@ -255,7 +257,7 @@ cosa_status cosa_page_map(int32_t batch, int32_t page_size, int32_t max_pages, c
   a.batch = batch;
   a.max_pages = max_pages;
   a.free_capacity = free_capacity;
-  a.max_new = max_new;
+  a.max_new = slots ? max_new : 0;
   a.cached = cached_lens;
   a.add = new_lens;
   a.free_pages = free_pages;

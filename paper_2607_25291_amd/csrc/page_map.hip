@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(PageMapArgs A) {
   __shared__ uint32_t waves[kThreads / 64];
   const uint32_t cap = (uint32_t)A.max_pages << A.log2_page;
   const uint32_t last = (1u << A.log2_page) - 1u;
-  const int n_free = min(max(*A.n_free, 0), A.free_capacity);
+  const int n_free = A.batch ? min(max(*A.n_free, 0), A.free_capacity) : 0;  // an empty batch may come without it
   for (int r = threadIdx.x; r < A.batch; r += kThreads) {
     cached[r] = min((uint32_t)max(A.cached[r], 0), cap);
     add[r] = (uint32_t)max(A.add[r], 0);
@@ -110,13 +110,13 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(PageMapArgs A) {
   }
   __syncthreads();
   if (blockIdx.x == 0) {
-    if (threadIdx.x == 0) A.cu_new[A.batch] = (int)rows;
+    if (threadIdx.x == 0 && A.cu_new) A.cu_new[A.batch] = (int)rows;
     // pages taken: the largest need that was met (needs grow along the requests)
 #pragma unroll
     for (int d = 32; d; d >>= 1) taken = max(taken, (uint32_t)__shfl_xor((int)taken, d, 64));
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = taken;
     __syncthreads();
-    if (threadIdx.x == 0) *A.n_taken = (int)max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+    if (threadIdx.x == 0 && A.n_taken) *A.n_taken = (int)max(max(waves[0], waves[1]), max(waves[2], waves[3]));
   }
 
   const uint32_t step = gridDim.x * kThreads, self = blockIdx.x * kThreads + threadIdx.x;
