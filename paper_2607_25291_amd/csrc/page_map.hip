@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void page_map_kernel(PageMapArgs A) {
   // Pages request r takes when its rows start at packed row `first`; fits: row width and slot range.
   const auto need = [&](int r, uint32_t first, bool& fits) -> uint32_t {
     const uint32_t c = cached[r], n = add[r];
-    fits = n <= cap - c && sat_add(first, n) <= (uint32_t)A.max_new;
+    fits = n <= cap - c && first + n <= (uint32_t)A.max_new;  // below 2^32; a sum held at 2^31 - 1 leaves no row
     return fits ? ((c + n + last) >> A.log2_page) - ((c + last) >> A.log2_page) : 0u;
   };
 

@@ -70,3 +70,25 @@ def test_an_empty_step_between_others_in_a_captured_append():
         t.cuda.synchronize()
         assert taken.item() == 0 and cu[0].item() == 0 and (slots == -1).all()
         assert not kc.any() and not vc.any()
+
+
+def test_rows_that_end_at_the_largest_number_of_rows():
+    """2^31 - 1 rows: a request whose rows end there fits; one that would start there adds nothing, although the prefix
+    sums stop at the same number."""
+    t = torch()
+    most = 2 ** 31 - 1
+    i32 = lambda x: t.tensor(x, dtype=t.int32, device="cuda")
+    print(f"[page map] {most} rows", flush=True)
+    slots = t.zeros(most, dtype=t.int64, device="cuda")
+    for new, lens, taken, last in (([most, 5], [0, 0], 0, [-1] * 3), ([most - 3, 3, 1], [0, 3, 0], 1, [48, 49, 50])):
+        n = len(new)
+        table, seq, cu = i32([[-7, -7]] * n), i32([-7] * n), i32([-7] * (n + 1))
+        count = i32([-7])
+        B.cosa_page_map(n, 16, 2, i32([0] * n), i32(new), i32([3, 1, 2]), 3, i32([3]), table, seq, cu, slots, most, count)
+        t.cuda.synchronize()
+        assert seq.tolist() == lens and count.item() == taken
+        assert cu.tolist() == [0] + [min(sum(new[:i + 1]), most) for i in range(n)]
+        assert table.tolist() == [[3 if x else -7, -7] for x in lens]
+        assert slots[-3:].tolist() == last
+        for a in range(0, most - 3, 2 ** 28):
+            assert (slots[a:min(a + 2 ** 28, most - 3)] == -1).all()
