@@ -482,8 +482,8 @@ def cosa_prefill_paged_varlen(problem, vl: CosaVarlen, q, kv: CosaPagedKv, sel: 
 # ---- decode-side operators (include/cosa_decode.h)
 
 def _place(stream, *tensors):
-    """Stream of a call (None: the current one of the device that holds the tensors) and the tensors' device
-    pointers. They must be contiguous and share one device; None and raw pointers pass through."""
+    """Stream of a call for _run (None: the current one of the device that holds the tensors) and the tensors'
+    device pointers. They must be contiguous and share one device; None and raw pointers pass through."""
     device, out = None, []
     for t in tensors:
         if t is not None and t.__class__ is not int:
@@ -505,18 +505,51 @@ def _same_device(d: int, device: Optional[int]) -> int:
     return d
 
 
-def _stream_of(stream, device: Optional[int]) -> Optional[int]:
+def _raw_stream(device: int) -> int:
+    # the handle alone: torch.cuda.current_stream() takes 1 us to build a Stream around it
+    global _raw_stream
+    import torch
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(device)
+
+
+def _get_device() -> int:
+    global _get_device
+    import torch
+    if not torch.cuda.is_available():
+        return 0
+    _get_device = torch._C._cuda_getDevice
+    return _get_device()
+
+
+def _stream_of(stream, device: Optional[int]):
+    """A stream's handle, or (handle, device) where that device has to be made current for the call."""
+    if device is None:
+        return _stream(stream)
     if stream is None:
+        handle = _raw_stream(device)
+    elif isinstance(stream, int):
+        handle = stream
+    else:
+        if stream.device.index != device:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{device}")
+        handle = stream.cuda_stream
+    # the null stream, the legacy and the per-thread one are those of whichever device is current
+    if handle <= 2 and device != _get_device():
+        return handle, device
+    return handle
+
+
+def _run(call, on, *args):
+    """Calls an entry point with its stream as the last argument."""
+    if on.__class__ is tuple:
         import torch
-        if device is None:
-            return torch.cuda.current_stream().cuda_stream
-        # the handle alone: torch.cuda.current_stream() takes 1 us to build a Stream around it
-        return torch._C._cuda_getCurrentRawStream(device)
-    if isinstance(stream, int):
-        return stream
-    if device is not None and stream.device.index != device:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{device}")
-    return stream.cuda_stream
+        with torch.cuda.device(on[1]):
+            status = call(*args, on[0])
+    else:
+        status = call(*args, on)
+    if status:
+        _check(status)
 
 
 def _rows(t, stride: int, like=None):
@@ -561,8 +594,8 @@ def cosa_page_map(batch: int, page_size: int, max_pages: int, cached_lens, new_l
                   n_taken, stream=None):
     s, (cached, new, free, nf, table, lens, cu, sl, taken) = _place(
         stream, cached_lens, new_lens, free_pages, n_free, page_table, seq_lens, cu_new, slots, n_taken)
-    _check(lib().cosa_page_map(batch, page_size, max_pages, cached, new, free, free_capacity, nf, table,
-                               lens, cu, sl, max_new, taken, s))
+    _run(lib().cosa_page_map, s, batch, page_size, max_pages, cached, new, free, free_capacity, nf, table,
+         lens, cu, sl, max_new, taken)
 
 
 def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, k_cache, v_cache,
@@ -573,21 +606,21 @@ def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int,
     s, (kc, vc, b, sl) = _place(stream, k_cache, v_cache, bounds, slots)
     kp, k_stride = _rows(k, k_stride, k_cache)
     vp, v_stride = _rows(v, v_stride, k_cache)
-    _check(lib().cosa_kv_append(n_kv_heads, head_dim, page_size, n_pages, kc, vc, b, n_tokens, kp,
-                                k_stride, vp, v_stride, sl, s))
+    _run(lib().cosa_kv_append, s, n_kv_heads, head_dim, page_size, n_pages, kc, vc, b, n_tokens, kp,
+         k_stride, vp, v_stride, sl)
 
 
 def cosa_page_score(problem, q, kv: CosaPagedKv, bounds, seq_lens, score, stream=None):
     s, (b, lens, out) = _place(stream, bounds, seq_lens, score)
     p, qp = _dprob(problem, q, score)
-    _check(lib().cosa_page_score(p, qp, _kvref(kv), b, lens, out, s))
+    _run(lib().cosa_page_score, s, p, qp, _kvref(kv), b, lens, out)
 
 
 def cosa_page_select(problem, page_size: int, seq_lens, score, budget: CosaPageBudget, pages, count,
                      stream=None):
     s, (lens, sc, pg, cnt) = _place(stream, seq_lens, score, pages, count)
     p, _ = _dprob(problem)
-    _check(lib().cosa_page_select(p, page_size, lens, sc, _kvref(budget), pg, cnt, s))
+    _run(lib().cosa_page_select, s, p, page_size, lens, sc, _kvref(budget), pg, cnt)
 
 
 def cosa_decode_workspace_bytes(problem) -> int:
@@ -602,7 +635,7 @@ def cosa_decode_attention(problem, q, kv: CosaPagedKv, seq_lens, workspace, work
                           lse=None, stream=None):
     s, (lens, ws, out, ls) = _place(stream, seq_lens, workspace, o, lse)
     p, qp = _dprob(problem, q, o)
-    _check(lib().cosa_decode_attention(p, qp, _kvref(kv), lens, ws, workspace_bytes, out, ls, s))
+    _run(lib().cosa_decode_attention, s, p, qp, _kvref(kv), lens, ws, workspace_bytes, out, ls)
 
 
 def cosa_decode_attention_listed(problem, q, kv: CosaPagedKv, seq_lens, pages, count,
@@ -610,8 +643,8 @@ def cosa_decode_attention_listed(problem, q, kv: CosaPagedKv, seq_lens, pages, c
                                  stream=None):
     s, (lens, pg, cnt, ws, out, ls) = _place(stream, seq_lens, pages, count, workspace, o, lse)
     p, qp = _dprob(problem, q, o)
-    _check(lib().cosa_decode_attention_listed(p, qp, _kvref(kv), lens, pg, cnt, list_pages, ws,
-                                              workspace_bytes, out, ls, s))
+    _run(lib().cosa_decode_attention_listed, s, p, qp, _kvref(kv), lens, pg, cnt, list_pages, ws,
+         workspace_bytes, out, ls)
 
 
 def cosa_decode_sparse_workspace_layout(problem, budget: CosaPageBudget) -> CosaDecodeSparseLayout:
@@ -629,5 +662,5 @@ def cosa_decode_sparse(problem, q, kv: CosaPagedKv, bounds, seq_lens, budget: Co
                        workspace, workspace_bytes: int, o, lse=None, stream=None):
     s, (b, lens, ws, out, ls) = _place(stream, bounds, seq_lens, workspace, o, lse)
     p, qp = _dprob(problem, q, o)
-    _check(lib().cosa_decode_sparse(p, qp, _kvref(kv), b, lens, _kvref(budget), ws, workspace_bytes,
-                                    out, ls, s))
+    _run(lib().cosa_decode_sparse, s, p, qp, _kvref(kv), b, lens, _kvref(budget), ws, workspace_bytes,
+         out, ls)

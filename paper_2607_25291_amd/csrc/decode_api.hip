@@ -15,12 +15,12 @@ using cosa::fail;
 using cosa::hip_fail;
 using cosa::ok;
 
-// Makes the device of `stream` current for the launches of one call (the null stream belongs to the current device).
+// Makes the device of `stream` current for the launches of one call (null, legacy and per-thread streams belong to the current device).
 class OnDevice {
  public:
   explicit OnDevice(hipStream_t stream) {
-    // the null stream and the per-thread one belong to whichever device is current
-    if (stream == nullptr || stream == hipStreamPerThread) return;
+    // the null stream, the legacy and the per-thread one belong to whichever device is current
+    if (stream == nullptr || stream == hipStreamLegacy || stream == hipStreamPerThread) return;
     hipDevice_t dev;
     if ((err_ = hipGetDevice(&before_)) != hipSuccess) return;
     if ((err_ = hipStreamGetDevice(stream, &dev)) != hipSuccess) return;
