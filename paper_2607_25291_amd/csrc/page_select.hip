@@ -58,7 +58,8 @@ __global__ __launch_bounds__(T) void page_select_kernel(PageSelectArgs A) {
   const int frac = (int)((A.fraction_micro * np + 999999) / 1000000);
   const int K = min(np, max(A.sink + A.recent, min(A.max_keep, max(A.min_keep, frac))));
   if (threadIdx.x == 0) A.count[u] = K;
-  for (int j = K + threadIdx.x; j < A.max_keep; j += T) out[j] = -1;
+  // unsigned: a list may be as wide as 2^31 - 1
+  for (uint32_t j = (uint32_t)K + threadIdx.x; j < (uint32_t)A.max_keep; j += T) out[j] = -1;
   if (K == np) {
     for (int j = threadIdx.x; j < K; j += T) out[j] = j;
     return;
