@@ -166,7 +166,7 @@ hipError_t launch_page_map(const PageMapArgs& a, hipStream_t stream) {
     }
   }
   // A workgroup for every 512 rows, so that the scan it starts with is a small part of a large map.
-  const int grid = std::min(std::max((a.max_new + 511) / 512, 1), 512);
+  const int grid = std::min(std::max(a.max_new / 512 + (a.max_new % 512 != 0), 1), 512);
   hipLaunchKernelGGL(page_map_kernel, dim3(grid), dim3(kThreads), lds, stream, a);
   return hipGetLastError();
 }
