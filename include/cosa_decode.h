@@ -175,7 +175,8 @@ size_t cosa_decode_sparse_workspace_bytes(const cosa_decode_problem* problem,
 
 /*
  * cosa_page_score, cosa_page_select and cosa_decode_attention_listed back to back on one stream,
- * bit-identical to those calls; their results stay in the workspace at the layout's offsets.
+ * bit-identical to those calls; their results stay in the workspace at the layout's offsets. A budget above the
+ * table's max_pages keeps at most those, so min(budget->max_pages, max_pages) * page_size < 2^31 is enough.
  */
 cosa_status cosa_decode_sparse(const cosa_decode_problem* problem, const void* q,
                                const cosa_paged_kv* kv, const void* bounds,

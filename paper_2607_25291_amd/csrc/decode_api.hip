@@ -2,6 +2,8 @@
 // launches. Every entry point validates all arguments before enqueuing anything.
 #include <math.h>
 
+#include <algorithm>
+
 #include "api_status.h"
 #include "cosa_decode.h"
 #include "decode_internal.h"
@@ -417,7 +419,8 @@ cosa_status cosa_decode_sparse(const cosa_decode_problem* problem, const void* q
   int64_t micro = 0;
   cosa_decode_sparse_layout l;
   if ((st = sparse_layout(problem, budget, any, micro, empty, l)) != COSA_OK) return st;
-  if ((st = check_tokens(sh, budget->max_pages)) != COSA_OK) return st;
+  // a list holds no more pages than the table
+  if ((st = check_tokens(sh, std::min(budget->max_pages, sh.max_pages))) != COSA_OK) return st;
   if ((st = check_score_space(sh)) != COSA_OK) return st;
   if (empty) return ok();
   if ((st = check_q(q)) != COSA_OK) return st;

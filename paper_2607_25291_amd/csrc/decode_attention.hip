@@ -522,7 +522,8 @@ bool decode_fits(const DecodeShape& sh, long long tokens) {
 
 hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, hipStream_t stream) {
   const bool listed = a.pages != nullptr;
-  const long long tokens = listed ? (long long)a.list_pages << sh.log2_page : sh.cap();
+  // Selected lists are wider than 2^31 tokens only by entries that their counts never reach.
+  const long long tokens = listed ? std::min((long long)a.list_pages << sh.log2_page, 0x7fffffffll) : sh.cap();
   const int nq = sh.G > 16 && (long long)sh.B * sh.Hkv * ((tokens + kTile - 1) / kTile) > kGrid<1> ? 2 : 1;
   const int QG = groups(sh.G, nq);
   int2* rec = static_cast<int2*>(a.workspace);

@@ -98,3 +98,18 @@ def test_default_streams_are_those_of_the_tensors_device(two_gpus, device, strea
             assert handle == 1 << 20, name
         else:
             assert (current, handle) == (device, 0), name
+
+
+def test_a_budget_above_the_tables_width_is_no_longer_list():
+    """cosa_decode_sparse: a list holds at most the table's pages, so a larger budget is neither too long nor too much
+    work; the lists' memory is what it asks for."""
+    def call(budget, max_pages=32, page=64, ws=None, batch=4):
+        B.cosa_decode_sparse(B.DecodeProblem(batch, 8, 2, max_pages), 16, B.CosaPagedKv(16, 16, 16, page, 16), 16, 16, budget,
+                             ws, 0, 1 << 30, stream=0)
+    for page, pages in ((64, 1 << 25), (1 << 20, 1 << 11), (16, 2 ** 31 - 1), (1 << 20, 2 ** 31 - 1)):
+        # everything is right but the workspace
+        refused(B.COSA_ERR_WORKSPACE, call, B.page_budget(pages), page=page)
+        refused(B.COSA_ERR_WORKSPACE, call, B.page_budget(pages), page=page, max_pages=0)
+        call(B.page_budget(pages), page=page, batch=0)
+    # where the table is as wide, the limits are its own
+    refused(B.COSA_ERR_UNSUPPORTED, call, B.page_budget(1 << 11), page=1 << 20, max_pages=1 << 11)
