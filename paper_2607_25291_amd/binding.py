@@ -552,22 +552,29 @@ def _run(call, on, *args):
         _check(status)
 
 
-def _rows(t, stride: int, like=None):
+def _rows(t, stride: int, like=None, want=None):
     """Pointer and row stride (elements) of rows [n, heads, head_dim]: a tensor whose rows are dense
-    but may lie apart, on the device of the tensor `like`, or a raw pointer with the given stride."""
+    but may lie apart, on the device of the tensor `like`, or a raw pointer with the given stride.
+    want: the rows (at least), heads and head_dim that a call reads."""
     if t is None or isinstance(t, int):
         return t, stride
     _same_device(t.get_device(), None if like is None or isinstance(like, int) else like.get_device())
-    if t.dim() != 3:
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError("rows must be [n, heads, head_dim]")
-    n, heads, dim = t.shape
-    row, head, elem = t.stride()
-    if (elem != 1 and dim > 1) or (head != dim and heads > 1):
-        raise ValueError("rows must be dense in heads and head_dim")
-    if n <= 1:
-        row = heads * dim
-    if row < heads * dim:
-        raise ValueError("rows must not overlap")
+    n, heads, dim = shape
+    if want is not None and (n < want[0] or heads != want[1] or dim != want[2] or t.element_size() != 2):
+        raise ValueError(f"rows of {want[1]} heads of {want[2]} bf16 elements (or their bits), at least {want[0]} of "
+                         f"them, expected; got {tuple(shape)} of {t.dtype}")
+    row = heads * dim
+    if not t.is_contiguous():
+        apart, head, elem = t.stride()
+        if (elem != 1 and dim > 1) or (head != dim and heads > 1):
+            raise ValueError("rows must be dense in heads and head_dim")
+        if n > 1:
+            if apart < row:
+                raise ValueError("rows must not overlap")
+            row = apart
     if stride and stride != row and n > 1:
         raise ValueError(f"row stride {stride} given for a tensor with row stride {row}")
     return t.data_ptr(), row
@@ -576,7 +583,7 @@ def _rows(t, stride: int, like=None):
 def _dprob(problem, q=None, like=None):
     """C problem and query pointer; the query tensor's own row stride goes into the problem."""
     p = problem.c if isinstance(problem, DecodeProblem) else problem
-    ptr, stride = _rows(q, p.q_stride, like)
+    ptr, stride = _rows(q, p.q_stride, like, (p.batch, p.n_q_heads, p.head_dim))
     if stride != p.q_stride and stride != p.n_q_heads * p.head_dim:
         p = CosaDecodeProblem(p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, p.max_pages, stride,
                               p.sm_scale)
@@ -601,11 +608,12 @@ def cosa_page_map(batch: int, page_size: int, max_pages: int, cached_lens, new_l
 def cosa_kv_append(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, k_cache, v_cache,
                    bounds, n_tokens: int, k, v, slots, k_stride: int = 0, v_stride: int = 0,
                    stream=None):
-    """k and v: [n_tokens, n_kv_heads, head_dim] tensors, slices of a fused projection among them
+    """k and v: [n_tokens (or more), n_kv_heads, head_dim] tensors, slices of a fused projection among them
     (their row strides are taken from the tensors)."""
     s, (kc, vc, b, sl) = _place(stream, k_cache, v_cache, bounds, slots)
-    kp, k_stride = _rows(k, k_stride, k_cache)
-    vp, v_stride = _rows(v, v_stride, k_cache)
+    want = (n_tokens, n_kv_heads, head_dim)
+    kp, k_stride = _rows(k, k_stride, k_cache, want)
+    vp, v_stride = _rows(v, v_stride, k_cache, want)
     _run(lib().cosa_kv_append, s, n_kv_heads, head_dim, page_size, n_pages, kc, vc, b, n_tokens, kp,
          k_stride, vp, v_stride, sl)
 

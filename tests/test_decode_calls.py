@@ -113,3 +113,36 @@ def test_a_budget_above_the_tables_width_is_no_longer_list():
         call(B.page_budget(pages), page=page, batch=0)
     # where the table is as wide, the limits are its own
     refused(B.COSA_ERR_UNSUPPORTED, call, B.page_budget(1 << 11), page=1 << 20, max_pages=1 << 11)
+
+
+def test_rows_that_are_not_the_problems(two_gpus):
+    """Query, key and value tensors must hold the rows that the call reads: its heads and head_dim, at least its sequences
+    or tokens, two bytes an element."""
+    import torch
+    z = lambda *s, dt=torch.bfloat16: Cuda(torch.zeros(*s, dtype=dt))
+    t = Cuda(torch.zeros(4, dtype=torch.int32))
+    good = z(4, 8, 128)
+    all_calls(t, good)
+    all_calls(t, z(6, 8, 128))                     # padded
+    all_calls(t, Cuda(torch.zeros(4, 24, 128, dtype=torch.int16)[:, 8:16]))
+    p, kv, b = B.DecodeProblem(4, 8, 8, 32), B.CosaPagedKv(16, 16, 16, 64, 16), B.page_budget(8)
+    calls = [lambda q: B.cosa_kv_append(8, 128, 64, 16, t, t, t, 4, q, good, t),
+             lambda q: B.cosa_kv_append(8, 128, 64, 16, t, t, t, 4, good, q, t),
+             lambda q: B.cosa_page_score(p, q, kv, t, t, t),
+             lambda q: B.cosa_decode_attention(p, q, kv, t, t, 64, t),
+             lambda q: B.cosa_decode_attention_listed(p, q, kv, t, t, t, 8, t, 64, t),
+             lambda q: B.cosa_decode_sparse(p, q, kv, t, t, b, t, 64, t)]
+    n = len(two_gpus["calls"])
+    for call in calls:
+        for bad in (z(3, 8, 128), z(4, 24, 128), z(4, 4, 128), z(4, 8, 64), z(4, 8, 256), z(4, 1024),
+                    z(4, 8, 128, dt=torch.float32), z(4, 8, 128, dt=torch.uint8)):
+            with pytest.raises(ValueError):
+                call(bad)
+    assert len(two_gpus["calls"]) == n
+    # a raw C problem says the same, and raw pointers pass
+    raw = B.CosaDecodeProblem(4, 8, 8, 128, 32, 0, 0.0)
+    B.cosa_page_score(raw, good, kv, t, t, t)
+    B.cosa_page_score(raw, 16, kv, t, t, t)
+    with pytest.raises(ValueError):
+        B.cosa_page_score(raw, z(4, 24, 128), kv, t, t, t)
+    B.cosa_kv_append(8, 128, 64, 16, t, t, t, 0, z(0, 8, 128), z(0, 8, 128), t)
