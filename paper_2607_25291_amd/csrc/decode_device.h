@@ -24,7 +24,7 @@ __device__ __forceinline__ u32x4_t ldg16_once(const void* p) {
 // r, columns 32 c + 8 gq .. + 7. Read that way, a load would take half a line of each row. So load (p, m) takes
 // line m of rows 8 p + r % 8 (16 bytes per lane, the third bit of the chunk in lane bit 3), and
 // to_operands() exchanges lane bit 3 with p: two DPP moves for two registers.
-template <int N, bool ONCE>
+template <int N>
 struct RowOperands {
   u32x4_t x[2 * N];
 
@@ -35,7 +35,7 @@ struct RowOperands {
     for (int p = 0; p < 2; ++p) {
       const uint16_t* a = row(8 * p + (r & 7)) + (r >> 3) * 32 + gq * 8;
 #pragma unroll
-      for (int m = 0; m < N; ++m) x[2 * m + p] = ONCE ? ldg16_once(a + m * 64) : ldg16(a + m * 64);
+      for (int m = 0; m < N; ++m) x[2 * m + p] = ldg16_once(a + m * 64);
     }
   }
   __device__ __forceinline__ void to_operands() {

@@ -22,8 +22,11 @@ struct ScoreParams {
 
 // A wave scores 16 pages. Waves that follow each other take the KV heads of the same pages, so that a page's
 // bounds, contiguous over its heads, are read at about one time. Lengths, table entries and queries are loaded
-// side by side: a table entry is read before it is known to be in use.
-template <bool ONCE, int NQ>
+// side by side: a table entry is read before it is known to be in use. Bounds are read with loads that the caches do not
+// keep: between two calls on a layer's bounds a step reads those of all other layers. Layers in turn with 1 / 32 / 64 / 128 /
+// 489 MB of bounds each, 3 GB in all (64 MB with 1 MB): 3.1 / 8.6 / 15.4 / 26.3 / 104 us a call, with loads that are
+// kept 2.9 / 9.1 / 16.5 / 29.4 / 105.
+template <int NQ>
 __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
   const int lane = threadIdx.x, r = lane & 15, gq = lane >> 4;
   const int id = blockIdx.x;
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) qf[y][c] = ldg16(q + (size_t)h * kHeadDim + c * 32);
   }
-  RowOperands<4, ONCE> x;  // minimum, then maximum
+  RowOperands<4> x;  // minimum, then maximum
   x.load(lane, [&](int k) __attribute__((always_inline)) {
     const size_t pg = (unsigned)__shfl(page_of_lane, k, 64);
     return P.bounds + (pg * P.Hkv + g) * 2 * kHeadDim;
@@ -81,12 +84,6 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
   }
 }
 
-template <bool ONCE>
-void launch_t(const ScoreParams& P, int n_waves, hipStream_t stream) {
-  if (P.G > 16) hipLaunchKernelGGL((page_score_kernel<ONCE, 2>), dim3(n_waves), dim3(64), 0, stream, P);
-  else hipLaunchKernelGGL((page_score_kernel<ONCE, 1>), dim3(n_waves), dim3(64), 0, stream, P);
-}
-
 }  // namespace
 
 hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uint16_t* bounds,
@@ -97,11 +94,8 @@ hipError_t launch_page_score(const DecodeShape& sh, const uint16_t* q, const uin
   const ScoreParams P{q, bounds, table, seq_lens, score, sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages,
                       sh.log2_page, segs, sh.q_stride, sh.n_pages, sh.scale,
                       sh.max_pages % 4 == 0 && reinterpret_cast<uintptr_t>(score) % 16 == 0};
-  // Bounds that fit the 256 MB of the last-level cache may still be there from the step before: plain loads keep
-  // them (75 MB: 23.4 us, 25.2 with loads that do not). Larger ones only push others out (307 MB: 76.9 us
-  // and 74.7).
-  if (sh.n_pages * sh.Hkv * (4 * kHeadDim) <= 256ll << 20) launch_t<false>(P, n_waves, stream);
-  else launch_t<true>(P, n_waves, stream);
+  if (sh.G > 16) hipLaunchKernelGGL((page_score_kernel<2>), dim3(n_waves), dim3(64), 0, stream, P);
+  else hipLaunchKernelGGL((page_score_kernel<1>), dim3(n_waves), dim3(64), 0, stream, P);
   return hipGetLastError();
 }
 
