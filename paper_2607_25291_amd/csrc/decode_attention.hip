@@ -107,7 +107,7 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&term)[3]
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint16_t* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, bytes, 0x00020000);
 }
-constexpr int kOnce = 2;  // cache policy of a buffer load: read once (ldg16_once)
+constexpr int kOnce = 2;  // cache policy of a buffer load: read once, not kept
 
 struct Tile {
   u32x4_t k[2][4], v[8];

@@ -14,19 +14,19 @@ __device__ __forceinline__ f32x4_t mfma16(const u32x4_t& a, const u32x4_t& b, co
 }
 
 // 16 bytes that a step reads once: not kept in the caches behind others that are read again. A kernel that only
-// reads 4.3 GB: 6.13 TB/s with plain loads, 7.05 TB/s with these. A load instruction must cover whole 128-byte lines,
-// or they are fetched twice.
+// reads 4.3 GB: 6.13 TB/s with plain loads, 7.05 TB/s with these.
 __device__ __forceinline__ u32x4_t ldg16_once(const void* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
 }
 
-// MFMA operands of 16 rows of N * 64 bf16 at `row(i)`, for rows as lanes: operand c (32 columns) of lane (r, gq) is row
-// r, columns 32 c + 8 gq .. + 7. Read that way, a load would take half a line of each row. So load (p, m) takes
-// line m of rows 8 p + r % 8 (16 bytes per lane, the third bit of the chunk in lane bit 3), and
-// to_operands() exchanges lane bit 3 with p: two DPP moves for two registers.
-template <int N>
+// MFMA operands of 16 rows of 256 bf16 at `row(i)`, read once, for rows as lanes: operand c (32 columns) of lane (r, gq)
+// is row r, columns 32 c + 8 gq .. + 7. Read that way, a load instruction would take half a line of 128 bytes of
+// each row, and a line that is not kept would be fetched twice. So load (p, m) takes line m of rows 8 p + r % 8 (16
+// bytes per lane, the third bit of the chunk in lane bit 3), and to_operands() exchanges lane bit 3 with p:
+// two DPP moves for two registers.
 struct RowOperands {
-  u32x4_t x[2 * N];
+  static constexpr int kLines = 4;
+  u32x4_t x[2 * kLines];
 
   template <class Row>
   __device__ __forceinline__ void load(int lane, Row&& row) {
@@ -35,12 +35,12 @@ struct RowOperands {
     for (int p = 0; p < 2; ++p) {
       const uint16_t* a = row(8 * p + (r & 7)) + (r >> 3) * 32 + gq * 8;
 #pragma unroll
-      for (int m = 0; m < N; ++m) x[2 * m + p] = ldg16_once(a + m * 64);
+      for (int m = 0; m < kLines; ++m) x[2 * m + p] = ldg16_once(a + m * 64);
     }
   }
   __device__ __forceinline__ void to_operands() {
 #pragma unroll
-    for (int m = 0; m < N; ++m)
+    for (int m = 0; m < kLines; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int a = (int)x[2 * m][i], b = (int)x[2 * m + 1][i];

@@ -64,7 +64,7 @@ struct DecodeArgs {
   uint16_t* o;
   float* lse;  // optional
 };
-// Scratch of a decode attention call. 0: too large for one launch.
+// Scratch of a decode attention call that decode_fits.
 size_t decode_workspace_bytes(const DecodeShape& sh);
 // Whether the units and tiles of a call (capacity `tokens` per sequence and KV head) fit a grid and 31 bits.
 bool decode_fits(const DecodeShape& sh, long long tokens);

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64) void page_score_kernel(ScoreParams P) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) qf[y][c] = ldg16(q + (size_t)h * kHeadDim + c * 32);
   }
-  RowOperands<4> x;  // minimum, then maximum
+  RowOperands x;  // minimum, then maximum
   x.load(lane, [&](int k) __attribute__((always_inline)) {
     const size_t pg = (unsigned)__shfl(page_of_lane, k, 64);
     return P.bounds + (pg * P.Hkv + g) * 2 * kHeadDim;
