@@ -58,7 +58,7 @@ struct DecodeParams {
   int max_pages, log2_page, list_pages;
   int items, mult;  // items of equal tile counts in a row: sequences (mult Hkv * QG) or KV heads (mult QG)
   long long q_stride, n_pages;
-  float scale_log2;
+  float scale, scale_log2;  // of logits: natural, and for exp2
 };
 
 __device__ __forceinline__ float xmax16(float v) { return fmaxf(v, __shfl_xor(v, 16, 64)); }
@@ -125,7 +125,9 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
 
   u32x4_t qf[NQ][4];
   f32x4_t acc[NQ][8];
-  float m[NQ], l[NQ];  // running maximum (log2 units) of column r, and this lane's share of its sum
+  // Running maximum of column r and this lane's share of its sum. Maxima are kept without the scale, and differences
+  // taken before it: a scaled one's rounding, 2^-24 of it, would be a factor of every weight (above 2^31, infinity or 0).
+  float m[NQ], l[NQ];
 #pragma unroll
   for (int x = 0; x < NQ; ++x) {
     const uint16_t* q =
@@ -210,14 +212,14 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
       }
       float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                        fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-      mx = half_max(xmax16(mx)) * P.scale_log2;
+      mx = half_max(xmax16(mx));
       const float mn = fmaxf(m[x], mx);
       const float base = mn == -INFINITY ? 0.f : mn;
-      const float alpha = __builtin_amdgcn_exp2f(m[x] - base);
+      const float alpha = __builtin_amdgcn_exp2f((m[x] - base) * P.scale_log2);
       float p[8], sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], P.scale_log2, -base));
+        p[i] = __builtin_amdgcn_exp2f((s[i >> 2][i & 3] - base) * P.scale_log2);
         sum += p[i];
       }
       l[x] = l[x] * alpha + sum;
@@ -297,7 +299,7 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
     float L = 0.f, O = 0.f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      const float a = __builtin_amdgcn_exp2f(sm[i][hh] - base);
+      const float a = __builtin_amdgcn_exp2f((sm[i][hh] - base) * P.scale_log2);
       L += a * sl[i][hh];
       O += a * so[i][hh][d];
     }
@@ -312,7 +314,7 @@ __device__ __forceinline__ void walk(const DecodeParams& P, int n, int g, int qg
       // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
       const __bf16 v = (__bf16)(L == 0.f ? 0.f : O / L);
       P.o[out * kHeadDim + d] = __builtin_bit_cast(uint16_t, v);
-      if (P.lse && d == 0) P.lse[out] = L == 0.f ? -INFINITY : M * 0.6931471805599453f + logf(L);
+      if (P.lse && d == 0) P.lse[out] = L == 0.f ? -INFINITY : M * P.scale + logf(L);
     }
   }
   __syncthreads();  // so, sm and sl are used again
@@ -444,7 +446,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   f32x4_t O = {0.f, 0.f, 0.f, 0.f};
   const auto add = [&](float m, float l, const f32x4_t& o) {
     const float mx = fmaxf(M, m), base = mx == -INFINITY ? 0.f : mx;
-    const float a = __builtin_amdgcn_exp2f(M - base), b = __builtin_amdgcn_exp2f(m - base);
+    const float a = __builtin_amdgcn_exp2f((M - base) * P.scale_log2), b = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
     L = a * L + b * l;
     O = a * O + b * o;
     M = mx;
@@ -479,7 +481,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(DecodeParams P, int 
   for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint16_t, (__bf16)(L == 0.f ? 0.f : O[i] / L));
   *reinterpret_cast<u32x2_t*>(P.o + out * kHeadDim + t * 4) =
       u32x2_t{o[0] | (uint32_t)o[1] << 16, o[2] | (uint32_t)o[3] << 16};
-  if (P.lse && t == 0) P.lse[out] = L == 0.f ? -INFINITY : M * 0.6931471805599453f + logf(L);
+  if (P.lse && t == 0) P.lse[out] = L == 0.f ? -INFINITY : M * P.scale + logf(L);
 }
 
 template <bool LISTED, int NQ>
@@ -531,7 +533,7 @@ hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, h
   const DecodeParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.pages, a.count, part, rec, a.o, a.lse,
                        sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages, sh.log2_page, a.list_pages,
                        listed ? sh.B * sh.Hkv : sh.B, listed ? QG : sh.Hkv * QG, sh.q_stride, sh.n_pages,
-                       sh.scale * 1.4426950408889634f};
+                       sh.scale, sh.scale * 1.4426950408889634f};
   if (nq == 1) return listed ? launch_t<true, 1>(P, tokens, stream) : launch_t<false, 1>(P, tokens, stream);
   return listed ? launch_t<true, 2>(P, tokens, stream) : launch_t<false, 2>(P, tokens, stream);
 }

@@ -6,9 +6,10 @@ import numpy as np
 import pytest
 
 from oracle import decode_oracle as D
+from oracle.cosa_oracle import widen
 from paper_2607_25291_amd import binding as B
 from paper_2607_25291_amd.inputs import f32_to_bf16_bits
-from tests.decode_util import Cache, as_f64, check_attention, run_decode
+from tests.decode_util import Cache, as_f64, check_attention, normal, run_decode
 from tests.gpu_util import dev
 
 pytestmark = pytest.mark.gpu
@@ -110,3 +111,48 @@ def test_infinite_values(name, listed):
     assert np.array_equal(got[odd], ro[odd], equal_nan=True)
     wt[odd] = ro[odd] = got[odd] = 0
     check_attention(got, lse.cpu().numpy().astype(np.float64), (ro, rl, wt, mag), max(lens))
+
+
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 60])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_large_logits(name, scale, listed):
+    """Logits of +-2^33 (1 + j / 128), apart by 2^26 at least where they differ (and 2^60 times as large): only the tokens
+    of the largest have weight, 1 each, in every head. o is the mean of at most three values: nine products of their
+    weights' terms in fp32 (2^-24 of the magnitudes for each, 2^-20 with room), and a rounding to bf16 (2^-9 of it, taken
+    as 2^-8 with the division). lse: the logit times the scale is exact, plus log(n) of at most log 3: half a unit of
+    fp32, 2^-24 of it."""
+    lens, hq, hkv, page, width = SHAPES[name]
+    say(f"[decode large logits] {name} scale {scale} listed {listed}")
+    rng = np.random.default_rng(len(name) + 3)
+    c, q = few_elements(rng, lens, hq, hkv, page, width)
+    q[:, :, 0] = 0x4980  # 2^20
+    q[:, :, 1] = 0
+    want, mag = np.zeros((2, len(lens), hq, 128))
+    best = np.zeros((len(lens), hq))
+    for n, length in enumerate(lens):
+        sign = -1.0 if n % 2 else 1.0
+        for h in range(hkv):
+            j = rng.integers(0, 100, length)
+            top = 100 if sign > 0 else -1
+            at = rng.choice(length, int(rng.integers(1, 4)), replace=False)
+            j[at] = top
+            k = (sign * 2.0 ** 13 * (1 + (j + 1) / 128)).astype(np.float32)
+            v = normal(rng, length, 128)
+            i = np.arange(length)
+            c.k[c.table[n, i // page], h, i % page, 0] = f32_to_bf16_bits(k)
+            c.v[c.table[n, i // page], h, i % page] = v
+            g = hq // hkv
+            want[n, h * g:(h + 1) * g] = widen(v[at]).mean(0)
+            mag[n, h * g:(h + 1) * g] = np.abs(widen(v[at])).mean(0)
+            best[n, h * g:(h + 1) * g] = 2.0 ** 20 * float(k.max()) * scale + np.log(len(at))
+            assert (widen(f32_to_bf16_bits(k)) == k).all() and (k == k.max()).sum() == len(at)
+    p = B.DecodeProblem(len(lens), hq, hkv, c.width, sm_scale=scale)
+    lists = None
+    if listed:
+        pages = np.tile(np.arange(c.width, dtype=np.int32), (len(lens), hkv, 1))
+        lists = (pages, np.array([[-(-n // page)] * hkv for n in lens], np.int32))
+    o, lse = run_decode(p, c, dev(q), lists)
+    got = as_f64(o)
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * mag).all()
+    assert (np.abs(lse.cpu().numpy() - best) <= 2.0 ** -24 * np.abs(best)).all()
