@@ -25,7 +25,9 @@
  *     multiples of 8 elements.
  *
  * Supported problem space (COSA_ERR_UNSUPPORTED otherwise): head_dim == 128, page_size a power of two
- * in [16, 2^20], max_pages * page_size < 2^31.
+ * in [16, 2^20], max_pages * page_size < 2^31, and what one launch holds. With U = batch * n_kv_heads * ceil(G / 16)
+ * for G query heads per KV head: U < 2^22 in every call with a problem, U * (tiles of 128 tokens in a table row or list + 1) < 2^31
+ * in attention, U * ceil(max_pages / 16) < 2^26 in page scores, n_tokens * n_kv_heads <= 2^29 in an append.
  */
 #ifndef COSA_DECODE_H_
 #define COSA_DECODE_H_
@@ -105,8 +107,8 @@ cosa_status cosa_kv_append(int32_t n_kv_heads, int32_t head_dim, int32_t page_si
 /*
  * Upper bound on the logits of every page (the cheap score of cosa_page_select):
  *   score[n, h, j] = sm_scale * sum_d max(q[n, h, d] * min[d], q[n, h, d] * max[d])
- * with min, max the bounds of page page_table[n, j] and KV head h / (Hq / Hkv): no key of the page has a
- * larger logit. score is fp32 [batch, n_q_heads, max_pages]; entries of pages that sequence n does not hold
+ * with min, max the bounds of page page_table[n, j] and KV head h / (Hq / Hkv): but for rounding, no key of
+ * the page has a larger logit. score is fp32 [batch, n_q_heads, max_pages]; entries of pages that sequence n does not hold
  * (j >= ceil(seq_lens[n] / page_size)) are not written. seq_lens is read as clamped to [0, max_pages * page_size]
  * (here and below). Only page_table, page_size and n_pages of kv are used. A page with an infinite or NaN
  * bound scores NaN or infinity. fp32 sums in a fixed order.
@@ -136,8 +138,9 @@ cosa_status cosa_page_select(const cosa_decode_problem* problem, int32_t page_si
  * exponentials. fp32 arithmetic; probabilities enter the product with V as three bf16 terms (all 24 bits). An
  * empty sequence, or one whose logits are all -inf, gives o = 0 and lse = -inf. An infinite v[t] gives that infinity in its
  * element (NaN beside one of the other sign, or where its weight is 0 or below 2^-100 of the largest); NaN values and
- * logits give NaN. What the cache holds behind seq_lens does not matter (NaN included). The tokens are split over a fixed grid and joined in a fixed order: results are
- * deterministic. The workspace is scratch of at least cosa_decode_workspace_bytes() bytes.
+ * logits give NaN. What the cache holds behind seq_lens does not matter (NaN included). The tokens are split over a
+ * fixed grid and joined in a fixed order: results are deterministic. The workspace is scratch of at least
+ * cosa_decode_workspace_bytes() bytes.
  */
 size_t cosa_decode_workspace_bytes(const cosa_decode_problem* problem);
 cosa_status cosa_decode_attention(const cosa_decode_problem* problem, const void* q,

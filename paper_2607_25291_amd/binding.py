@@ -558,7 +558,9 @@ def _rows(t, stride: int, like=None, want=None):
     want: the rows (at least), heads and head_dim that a call reads."""
     if t is None or isinstance(t, int):
         return t, stride
-    _same_device(t.get_device(), None if like is None or isinstance(like, int) else like.get_device())
+    d = t.get_device()
+    if d < 0 or (like is not None and like.__class__ is not int and like.get_device() != d):
+        _same_device(d, like.get_device() if d >= 0 else None)
     shape = t.shape
     if len(shape) != 3:
         raise ValueError("rows must be [n, heads, head_dim]")
