@@ -15,7 +15,7 @@
 // a second kernel joins them in order.
 //
 // Bound: HBM. A token costs 512 bytes per KV head and 4 G d flops, G flops per byte. 32 / 8 heads: one sequence of 128K
-// tokens (537 MB) 84 us and 4 us of joining, 64 of up to 64K (4.1 GB) 597 to 632 us, where a kernel that only reads
+// tokens (537 MB) 84 us and 4.5 us of joining, 64 of up to 64K (4.1 GB) 599 to 632 us, where a kernel that only reads
 // takes 85 and 584. Values are read with loads that the caches do not keep (128K: 105 us with events, 116
 // without); keys not (no gain, and 10 % slower where a short context stays in the last-level cache).
 #include "decode_device.h"

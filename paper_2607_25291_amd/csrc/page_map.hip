@@ -5,7 +5,7 @@
 // finding the request of an entry or a row by binary search. So one launch does it, with no pass between
 // the scan and its use.
 //
-// Bound: latency. 64 requests of one token 4.2 us, 256 prompts with 90K rows 6.5, 4096 / 8192 requests 14 / 22 (18 / 40
+// Bound: latency. 64 requests of one token 4.3 us, 256 prompts with 90K rows 6.5 to 7.3, 4096 / 8192 requests 14 / 22 (18 / 40
 // with the lengths read from memory in every pass).
 #include <mutex>
 

@@ -6,9 +6,11 @@
 // equal it are kept; a scan over the pages then packs the kept ones in ascending order, so the list needs
 // no sort.
 //
-// Bound: latency (the barriers between its steps). 256 rows of up to 4096 pages, 7 heads: 12.1 us for 8.7 MB; 8 rows
-// of 256 pages, 4 heads: 5.9 us, of which an empty launch takes 2. Comparing all pairs of 256 keys instead of
-// the radix selection: 14.2 us.
+// Bound: latency, the barriers between its steps, and for about a tenth the first digit: the differences span a few
+// binary exponents, so their pages crowd into a few tens of its bins. 256 rows of up to 4096 pages, 7 heads: 12.1 us
+// for 8.7 MB (events 17.6; 16.0 with differences over 240 exponents, 25.8 with all equal); 8 rows of 256 pages, 4
+// heads: 6.0 us, of which an empty launch takes 2. Comparing all pairs of 256 keys instead of the radix selection:
+// 14.2 us.
 #include <mutex>
 
 #include "cosa_device.h"
