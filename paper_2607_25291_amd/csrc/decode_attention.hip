@@ -18,6 +18,10 @@
 // tokens (537 MB) 84 us and 4.5 us of joining, 64 of up to 64K (4.1 GB) 599 to 632 us, where a kernel that only reads
 // takes 85 and 584. Values are read with loads that the caches do not keep (128K: 105 us with events, 116
 // without); keys not (no gain, and 10 % slower where a short context stays in the last-level cache).
+#include <float.h>
+
+#include <algorithm>
+
 #include "decode_device.h"
 #include "decode_internal.h"
 #include "decode_split.h"
@@ -533,7 +537,7 @@ hipError_t launch_decode_attention(const DecodeShape& sh, const DecodeArgs& a, h
   const DecodeParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.pages, a.count, part, rec, a.o, a.lse,
                        sh.Hq, sh.Hkv, sh.G, QG, sh.max_pages, sh.log2_page, a.list_pages,
                        listed ? sh.B * sh.Hkv : sh.B, listed ? QG : sh.Hkv * QG, sh.q_stride, sh.n_pages,
-                       sh.scale, sh.scale * 1.4426950408889634f};
+                       sh.scale, std::min(sh.scale * 1.4426950408889634f, FLT_MAX)};  // 0 times infinity is no logit
   if (nq == 1) return listed ? launch_t<true, 1>(P, tokens, stream) : launch_t<false, 1>(P, tokens, stream);
   return listed ? launch_t<true, 2>(P, tokens, stream) : launch_t<false, 2>(P, tokens, stream);
 }

@@ -156,3 +156,29 @@ def test_large_logits(name, scale, listed):
     got = as_f64(o)
     assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * mag).all()
     assert (np.abs(lse.cpu().numpy() - best) <= 2.0 ** -24 * np.abs(best)).all()
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_largest_scale(name):
+    """A scale whose product with log2(e) passes fp32: logits of 0 keep weight 1, any below them none; one or two tokens of
+    0 per sequence, lse log(1) or log(2) (half a unit of fp32)."""
+    lens, hq, hkv, page, width = SHAPES[name]
+    say(f"[decode largest scale] {name}")
+    rng = np.random.default_rng(len(name) + 5)
+    c, q = few_elements(rng, lens, hq, hkv, page, width)
+    want = np.zeros((len(lens), hq, 128))
+    count = np.array([1 + n % 2 for n in range(len(lens))])
+    for n, length in enumerate(lens):
+        i = np.arange(length)
+        at = rng.choice(length, count[n], replace=False)
+        k = -rng.uniform(1e-6, 1.0, length).astype(np.float32)
+        k[at] = 0
+        v = normal(rng, length, 128)
+        v[at] = v[at[:1]]
+        c.k[c.table[n, i // page], :, i % page, 0] = f32_to_bf16_bits(k)[:, None]
+        c.v[c.table[n, i // page], :, i % page] = v[:, None]
+        want[n] = widen(v[at[0]])
+    o, lse = run_decode(B.DecodeProblem(len(lens), hq, hkv, c.width, sm_scale=3e38), c, dev(q))
+    # the same value once or twice over as many: exact but for the order of its three terms' products (2^-22), one rounding
+    assert (np.abs(as_f64(o) - want) <= (2.0 ** -8 + 2.0 ** -22) * np.abs(want)).all()
+    assert (np.abs(lse.cpu().numpy() - np.log(count)[:, None]) <= 2.0 ** -23).all()
