@@ -17,6 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcosa.so")
 HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "cosa.h")
 DECODE_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "cosa_decode.h")
+SERVING_HEADER_PATH = os.path.join(os.path.dirname(_PKG), "include", "cosa_serving.h")
 
 COSA_OK, COSA_ERR_INVALID_ARG, COSA_ERR_UNSUPPORTED, COSA_ERR_WORKSPACE, COSA_ERR_HIP = range(5)
 SELECT_FRACTION, SELECT_TOP_P, SELECT_ALL = 0, 1, 2
@@ -78,6 +79,13 @@ class CosaDecodeSparseLayout(ctypes.Structure):
                 ("partial", ctypes.c_size_t), ("total", ctypes.c_size_t)]
 
 
+class CosaChunkProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("sm_scale", ctypes.c_float)]
+
+
 class CosaError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(message)
@@ -121,6 +129,25 @@ class DecodeProblem:
     def c(self) -> CosaDecodeProblem:
         return CosaDecodeProblem(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
                                  self.max_pages, self.q_stride, self.sm_scale)
+
+
+@dataclass(frozen=True)
+class ChunkProblem:
+    """New tokens of a batch of sequences (cosa_chunk_problem): n_rows packed query rows. q_stride 0: they are
+    dense, or a tensor passed as q brings its own stride."""
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    max_pages: int
+    n_rows: int
+    head_dim: int = 128
+    q_stride: int = 0
+    sm_scale: float = 0.0
+
+    @cached_property
+    def c(self) -> CosaChunkProblem:
+        return CosaChunkProblem(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
+                                self.max_pages, self.n_rows, self.q_stride, self.sm_scale)
 
 
 _lib = None
@@ -234,6 +261,11 @@ def lib():
         L.cosa_decode_sparse_workspace_bytes.argtypes = [D, PB]
         L.cosa_decode_sparse.restype = S
         L.cosa_decode_sparse.argtypes = [D, vp, KV, vp, vp, PB, vp, size, vp, vp, vp]
+        CH = ctypes.POINTER(CosaChunkProblem)
+        L.cosa_chunk_workspace_bytes.restype = size
+        L.cosa_chunk_workspace_bytes.argtypes = [CH]
+        L.cosa_chunk_attention.restype = S
+        L.cosa_chunk_attention.argtypes = [CH, vp, KV, vp, vp, vp, size, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -674,3 +706,31 @@ def cosa_decode_sparse(problem, q, kv: CosaPagedKv, bounds, seq_lens, budget: Co
     p, qp = _dprob(problem, q, o)
     _run(lib().cosa_decode_sparse, s, p, qp, _kvref(kv), b, lens, _kvref(budget), ws, workspace_bytes,
          out, ls)
+
+
+# ---- serving operators (include/cosa_serving.h)
+
+def _cprob(problem, q=None, like=None):
+    """C problem and query pointer; the query tensor's own row stride goes into the problem."""
+    p = problem.c if isinstance(problem, ChunkProblem) else problem
+    ptr, stride = _rows(q, p.q_stride, like, (p.n_rows, p.n_q_heads, p.head_dim))
+    if stride != p.q_stride and stride != p.n_q_heads * p.head_dim:
+        p = CosaChunkProblem(p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, p.max_pages, p.n_rows, stride,
+                             p.sm_scale)
+    return ctypes.byref(p), ptr
+
+
+def cosa_chunk_workspace_bytes(problem) -> int:
+    p, _ = _cprob(problem)
+    n = int(lib().cosa_chunk_workspace_bytes(p))
+    if n == 0:
+        raise CosaError(COSA_ERR_INVALID_ARG, cosa_last_error())
+    return n
+
+
+def cosa_chunk_attention(problem, q, kv: CosaPagedKv, seq_lens, cu_new, workspace, workspace_bytes: int, o,
+                         lse=None, stream=None):
+    """q: [n_rows (or more), n_q_heads, head_dim], a slice of a fused projection among them."""
+    s, (lens, cu, ws, out, ls) = _place(stream, seq_lens, cu_new, workspace, o, lse)
+    p, qp = _cprob(problem, q, o)
+    _run(lib().cosa_chunk_attention, s, p, qp, _kvref(kv), lens, cu, ws, workspace_bytes, out, ls)

@@ -4,80 +4,23 @@
 
 #include <algorithm>
 
-#include "api_status.h"
+#include "api_checks.h"
 #include "cosa_decode.h"
 #include "decode_internal.h"
 
 namespace {
 
 using cosa::align256;
-using cosa::as_stream;
+using cosa::check_n_pages;
+using cosa::check_page_size;
+using cosa::check_workspace;
 using cosa::DecodeShape;
 using cosa::fail;
-using cosa::hip_fail;
+using cosa::launch;
+using cosa::misaligned;
 using cosa::ok;
-
-// Makes the device of `stream` current for the launches of one call (null, legacy and per-thread streams belong to the current device).
-class OnDevice {
- public:
-  explicit OnDevice(hipStream_t stream) {
-    // the null stream, the legacy and the per-thread one belong to whichever device is current
-    if (stream == nullptr || stream == hipStreamLegacy || stream == hipStreamPerThread) return;
-    hipDevice_t dev;
-    if ((err_ = hipGetDevice(&before_)) != hipSuccess) return;
-    if ((err_ = hipStreamGetDevice(stream, &dev)) != hipSuccess) return;
-    if ((int)dev == before_) return;
-    err_ = hipSetDevice((int)dev);
-    moved_ = err_ == hipSuccess;
-  }
-  ~OnDevice() {
-    if (moved_) (void)hipSetDevice(before_);
-  }
-  OnDevice(const OnDevice&) = delete;
-  OnDevice& operator=(const OnDevice&) = delete;
-  hipError_t error() const { return err_; }
-
- private:
-  int before_ = 0;
-  bool moved_ = false;
-  hipError_t err_ = hipSuccess;
-};
-
-template <class F>
-cosa_status launch(void* stream, const char* what, F&& f) {
-  const hipStream_t s = as_stream(stream);
-  const OnDevice device(s);
-  hipError_t e = device.error();
-  if (e != hipSuccess) return hip_fail(e, "device of the stream");
-  e = f(s);
-  return e == hipSuccess ? ok() : hip_fail(e, what);
-}
-
-bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-
-// A range of memory that a call reads or writes.
-struct Span {
-  const void* p;
-  int64_t bytes;
-  bool meets(const Span& o) const {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
-    return p && o.p && bytes > 0 && o.bytes > 0 && a < b + (uintptr_t)o.bytes && b < a + (uintptr_t)bytes;
-  }
-};
-
-cosa_status check_page_size(int ps, int& log2_page) {
-  if (ps < 16 || ps > (1 << 20) || (ps & (ps - 1)) != 0)
-    return fail(COSA_ERR_INVALID_ARG, "page_size %d is not a power of two in [16, 2^20]", ps);
-  log2_page = 0;
-  while ((1 << log2_page) < ps) ++log2_page;
-  return ok();
-}
-
-cosa_status check_n_pages(int64_t n) {
-  if (n < 1 || n > (1ll << 31))
-    return fail(COSA_ERR_INVALID_ARG, "n_pages (%lld) outside [1, 2^31]", (long long)n);
-  return ok();
-}
+using cosa::Span;
+using cosa::u16;
 
 // Validates the problem; `empty` is set for batch == 0.
 cosa_status check_problem(const cosa_decode_problem* p, int page_size, DecodeShape& sh, bool& empty) {
@@ -160,12 +103,6 @@ cosa_status check_score_space(const DecodeShape& sh) {
   return ok();
 }
 
-cosa_status check_workspace(const void* ws, size_t bytes, size_t need) {
-  if (!ws || bytes < need) return fail(COSA_ERR_WORKSPACE, "workspace of %zu bytes at %p, need %zu", bytes, ws, need);
-  if (misaligned(ws, 16)) return fail(COSA_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-  return ok();
-}
-
 cosa_status check_q(const void* q) {
   if (!q || misaligned(q, 16)) return fail(COSA_ERR_INVALID_ARG, "q must be non-NULL and 16-byte aligned");
   return ok();
@@ -180,8 +117,6 @@ cosa_status check_o(const DecodeShape& sh, const void* q, const int32_t* seq_len
     return fail(COSA_ERR_INVALID_ARG, "o must not overlap q");
   return ok();
 }
-
-const uint16_t* u16(const void* p) { return static_cast<const uint16_t*>(p); }
 
 // Problem, cache and lengths of the attention calls, up to the workspace.
 cosa_status attention_shape(const cosa_decode_problem* problem, const cosa_paged_kv* kv, DecodeShape& sh, bool& empty) {
