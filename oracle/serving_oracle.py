@@ -50,3 +50,83 @@ def chunk_attention(q, k_cache, v_cache, table, lens, cu, sm_scale=0.0):
                         lse[a + i, hh] = m + np.log(total)
                         mag[a + i, hh] = big[i, seen].max()
     return o, lse, wt, mag
+
+
+def held(table, lens, page, n_pages):
+    """[(row, entry, page)] of the pages that rows hold; entries outside the cache are no pages."""
+    cap = table.shape[1] * page
+    out = []
+    for r in range(table.shape[0]):
+        for j in range(-(-min(max(int(lens[r]), 0), cap) // page)):
+            if 0 <= int(table[r, j]) < n_pages:
+                out.append((r, j, int(table[r, j])))
+    return out
+
+
+def page_fork(parent, table, lens, page, copy_all, free, n_free, new_table):
+    """Returns (new_table, new_lens, src, dst, rows): the lists as far as they are written."""
+    new_table = np.array(new_table, dtype=np.int64)
+    cap = table.shape[1] * page
+    n_free = min(max(int(n_free), 0), len(free))
+    has_child, lists, new_lens, needed = set(), [], [], 0
+    for c, p in enumerate(parent):
+        if not 0 <= p < len(lens):
+            new_lens.append(0)
+            continue
+        length = min(max(int(lens[p]), 0), cap)
+        pages, part = -(-length // page), length % page
+        fresh = None
+        if part and (copy_all or p in has_child):
+            needed += 1
+            if needed > n_free:
+                new_lens.append(0)
+                continue
+            fresh = int(free[needed - 1])
+            lists.append((int(table[p, pages - 1]), fresh, part))
+        has_child.add(p)
+        new_table[c, :pages] = table[p, :pages]
+        if fresh is not None:
+            new_table[c, pages - 1] = fresh
+        new_lens.append(length)
+    src, dst, rows = (np.array([x[i] for x in lists], dtype=np.int64) for i in range(3))
+    return new_table, np.array(new_lens, dtype=np.int64), src, dst, rows
+
+
+def page_copy(k_cache, v_cache, bounds, src, dst, rows, n):
+    """In place; caches [pages, Hkv, page, d], bounds [pages, Hkv, 2, d] or None, rows or None."""
+    n_pages, _, page, _ = k_cache.shape
+    for i in range(min(max(int(n), 0), len(src))):
+        s, d = int(src[i]), int(dst[i])
+        if not (0 <= s < n_pages and 0 <= d < n_pages):
+            continue
+        keep = page if rows is None else min(max(int(rows[i]), 0), page)
+        k_cache[d, :, :keep], v_cache[d, :, :keep] = k_cache[s, :, :keep], v_cache[s, :, :keep]
+        if bounds is not None:
+            bounds[d] = bounds[s]
+
+
+def page_release(old_table, old_lens, new_table, new_lens, page, n_pages, free, n_free, n_taken):
+    """The free list afterwards."""
+    n_free = min(max(int(n_free), 0), len(free))
+    left = [int(p) for p in free[min(max(int(n_taken), 0), n_free):n_free]]
+    old = {p for _, _, p in held(old_table, old_lens, page, n_pages)}
+    new = {p for _, _, p in held(new_table, new_lens, page, n_pages)}
+    return left + sorted(old - new - set(left))
+
+
+def page_compact(table, lens, page, n_pages, max_moves):
+    """Returns (new table, moves [(src, dst)], free list)."""
+    table = np.array(table, dtype=np.int64)
+    entries = held(table, lens, page, n_pages)
+    used = sorted({p for _, _, p in entries})
+    unused = sorted(set(range(n_pages)) - set(used))
+    moves = []
+    for s, d in zip(reversed(used), unused):
+        if d > s or len(moves) == max_moves:
+            break
+        moves.append((s, d))
+    to = dict(moves)
+    for r, j, p in entries:
+        table[r, j] = to.get(p, p)
+    now = {to.get(p, p) for p in used}
+    return table, moves, [p for p in range(n_pages) if p not in now]

@@ -266,6 +266,17 @@ def lib():
         L.cosa_chunk_workspace_bytes.argtypes = [CH]
         L.cosa_chunk_attention.restype = S
         L.cosa_chunk_attention.argtypes = [CH, vp, KV, vp, vp, vp, size, vp, vp, vp]
+        L.cosa_page_fork.restype = S
+        L.cosa_page_fork.argtypes = [i32, i32, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cosa_page_copy.restype = S
+        L.cosa_page_copy.argtypes = [i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+        L.cosa_page_workspace_bytes.restype = size
+        L.cosa_page_workspace_bytes.argtypes = [i64]
+        L.cosa_page_release.restype = S
+        L.cosa_page_release.argtypes = [i32, i32, i64, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, size,
+                                        vp]
+        L.cosa_page_compact.restype = S
+        L.cosa_page_compact.argtypes = [i32, i32, i32, i64, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, size, vp]
         _lib = L
     return _lib
 
@@ -734,3 +745,43 @@ def cosa_chunk_attention(problem, q, kv: CosaPagedKv, seq_lens, cu_new, workspac
     s, (lens, cu, ws, out, ls) = _place(stream, seq_lens, cu_new, workspace, o, lse)
     p, qp = _cprob(problem, q, o)
     _run(lib().cosa_chunk_attention, s, p, qp, _kvref(kv), lens, cu, ws, workspace_bytes, out, ls)
+
+
+def cosa_page_fork(n_parents: int, n_children: int, page_size: int, max_pages: int, parent, page_table, seq_lens,
+                   copy_all: int, free_pages, free_capacity: int, n_free, new_table, new_lens, src, dst, rows, n_taken,
+                   stream=None):
+    s, (par, table, lens, free, nf, nt, nl, a, b, r, taken) = _place(
+        stream, parent, page_table, seq_lens, free_pages, n_free, new_table, new_lens, src, dst, rows, n_taken)
+    _run(lib().cosa_page_fork, s, n_parents, n_children, page_size, max_pages, par, table, lens, copy_all, free,
+         free_capacity, nf, nt, nl, a, b, r, taken)
+
+
+def cosa_page_copy(n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, k_cache, v_cache, bounds, src, dst, rows,
+                   max_pairs: int, n_pairs, stream=None):
+    s, (kc, vc, b, a, d, r, n) = _place(stream, k_cache, v_cache, bounds, src, dst, rows, n_pairs)
+    _run(lib().cosa_page_copy, s, n_kv_heads, head_dim, page_size, n_pages, kc, vc, b, a, d, r, max_pairs, n)
+
+
+def cosa_page_workspace_bytes(n_pages: int) -> int:
+    n = int(lib().cosa_page_workspace_bytes(n_pages))
+    if n == 0:
+        raise CosaError(COSA_ERR_INVALID_ARG, cosa_last_error())
+    return n
+
+
+def cosa_page_release(page_size: int, max_pages: int, n_pages: int, old_batch: int, old_table, old_lens, new_batch: int,
+                      new_table, new_lens, free_pages, free_capacity: int, n_free, n_taken, free_out, out_capacity: int,
+                      n_free_out, workspace, workspace_bytes: int, stream=None):
+    s, (ot, ol, nt, nl, free, nf, taken, out, nfo, ws) = _place(
+        stream, old_table, old_lens, new_table, new_lens, free_pages, n_free, n_taken, free_out, n_free_out, workspace)
+    _run(lib().cosa_page_release, s, page_size, max_pages, n_pages, old_batch, ot, ol, new_batch, nt, nl, free,
+         free_capacity, nf, taken, out, out_capacity, nfo, ws, workspace_bytes)
+
+
+def cosa_page_compact(batch: int, page_size: int, max_pages: int, n_pages: int, page_table, seq_lens, max_moves: int,
+                      new_table, src, dst, n_moves, free_pages, free_capacity: int, n_free, workspace,
+                      workspace_bytes: int, stream=None):
+    s, (table, lens, nt, a, b, nm, free, nf, ws) = _place(
+        stream, page_table, seq_lens, new_table, src, dst, n_moves, free_pages, n_free, workspace)
+    _run(lib().cosa_page_compact, s, batch, page_size, max_pages, n_pages, table, lens, max_moves, nt, a, b, nm, free,
+         free_capacity, nf, ws, workspace_bytes)

@@ -21,7 +21,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libcosa.so")
 SOURCES = ["cosa_api.hip", "attention.hip", "kap_score.hip", "kap_select.hip", "block_mass.hip",
            "decode_api.hip", "page_map.hip", "kv_append.hip", "page_score.hip", "page_select.hip",
-           "decode_attention.hip", "serving_api.hip", "chunk_attention.hip"]
+           "decode_attention.hip", "serving_api.hip", "chunk_attention.hip", "page_fork.hip",
+           "page_copy.hip", "page_pool.hip"]
 
 ARCH = "gfx950"
 COMMON = [

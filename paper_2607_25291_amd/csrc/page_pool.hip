@@ -1,0 +1,377 @@
+// Pages given back to the free list, and pages moved to the lowest numbers, for gfx950.
+//
+// Both mark the pages that rows hold and then number the marked or unmarked ones in ascending order by a scan over the
+// cache's pages: no atomics whose order could show, and no state between calls. Few pages in few rows: one workgroup, with
+// the marks as bits in LDS. Otherwise kernels one after the other, with the marks as bytes in the workspace (plain
+// stores: a page marked twice gets the same byte twice): clear, mark, count by blocks, write.
+//
+// Bound: the launches' latency; the tables once (4 bytes an entry), the marks.
+#include <algorithm>
+
+#include "cosa_device.h"
+#include "select_wave.h"
+#include "serving_internal.h"
+
+namespace cosa {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlockPages = kThreads * 16;  // pages of a workgroup: 16 marks a thread
+constexpr int kEntries = 1024;              // table entries of a workgroup's turn
+
+struct Header {  // in the workspace, written by one kernel for the next ones
+  int a, b;
+};
+
+// The workspace: header, counts of the blocks, marks (release: two arrays of them), ranks (compact). Marks end with a
+// whole block.
+struct Pool {
+  Header* header;
+  int32_t* counts;
+  uint8_t *marks, *marks2;
+  int32_t* ranks;
+  int blocks;
+  size_t bytes;
+  Pool(void* ws, long long n_pages) {
+    blocks = (int)((n_pages + kBlockPages - 1) / kBlockPages);
+    char* p = static_cast<char*>(ws);
+    const size_t all = (size_t)blocks * kBlockPages, counts_at = 256, marks_at = counts_at + ((size_t)blocks * 4 + 255) / 256 * 256;
+    header = reinterpret_cast<Header*>(p);
+    counts = reinterpret_cast<int32_t*>(p + counts_at);
+    marks = reinterpret_cast<uint8_t*>(p + marks_at);
+    marks2 = marks + all;                                   // release
+    ranks = reinterpret_cast<int32_t*>(p + marks_at + all);  // compact
+    bytes = marks_at + 5 * all;
+  }
+};
+
+__device__ __forceinline__ int held_pages(int length, int max_pages, int log2_page) {
+  const uint32_t l = (uint32_t)min(max(length, 0), max_pages << log2_page);
+  return (int)((l + (1u << log2_page) - 1u) >> log2_page);
+}
+
+// Sum over the workgroup of one value per thread, and the sum of the threads in front. waves: NT / 64 words of LDS.
+template <int NT>
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* waves, uint32_t& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t at = wave_incl_scan(x, lane);
+  __syncthreads();  // waves may still be read from a scan before
+  if (lane == 63) waves[w] = at;
+  __syncthreads();
+  at -= x;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < NT / 64; ++i) {
+    if (i < w) at += waves[i];
+    total += waves[i];
+  }
+  return at;
+}
+
+__global__ __launch_bounds__(kThreads) void clear_kernel(u32x4_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) p[i] = u32x4_t{0, 0, 0, 0};
+}
+
+// f(page number) for the pages that workgroup turn x of a table holds: kEntries entries of one row.
+template <class F>
+__device__ __forceinline__ void for_held(const int32_t* table, const int32_t* lens, int max_pages, int log2_page,
+                                         long long n_pages, int x, F&& f) {
+  const int turns = (max_pages + kEntries - 1) / kEntries, row = x / turns, j0 = x % turns * kEntries;
+  const int j1 = min(j0 + kEntries, held_pages(lens[row], max_pages, log2_page));
+  for (int j = j0 + threadIdx.x; j < j1; j += kThreads) {
+    const int p = table[(size_t)row * max_pages + j];
+    if (p >= 0 && p < n_pages) f(p);
+  }
+}
+
+// ---- release
+
+__device__ __forceinline__ void free_list(const PageReleaseArgs& A, int& taken, int& n_free) {
+  n_free = min(max(*A.n_free, 0), A.free_capacity);
+  taken = A.n_taken ? min(max(*A.n_taken, 0), n_free) : 0;
+}
+
+// marks: pages that are held afterwards or listed already; marks2: pages that were held.
+__global__ __launch_bounds__(kThreads) void release_mark_kernel(PageReleaseArgs A, Pool W, int old_turns, int new_turns) {
+  const int all = old_turns + new_turns;
+  for (int x = blockIdx.x; x < all; x += gridDim.x) {
+    if (x < old_turns)
+      for_held(A.old_table, A.old_lens, A.max_pages, A.log2_page, A.n_pages, x, [&](int p) { W.marks2[p] = 1; });
+    else
+      for_held(A.new_table, A.new_lens, A.max_pages, A.log2_page, A.n_pages, x - old_turns, [&](int p) { W.marks[p] = 1; });
+  }
+  int taken, n_free;
+  free_list(A, taken, n_free);
+  for (int i = taken + blockIdx.x * kThreads + threadIdx.x; i < n_free; i += gridDim.x * kThreads) {
+    const int p = A.free_pages[i];
+    if (p >= 0 && p < A.n_pages) W.marks[p] = 1;
+    if (i - taken < A.out_capacity) A.free_out[i - taken] = p;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *W.header = Header{n_free - taken, 0};  // n_free_out may be n_free
+}
+
+// 16 marks of a thread as bits; release: the pages that become free.
+template <bool RELEASE>
+__device__ __forceinline__ uint32_t marks16(const Pool& W, int block) {
+  const size_t at = (size_t)block * kThreads + threadIdx.x;
+  u32x4_t m = reinterpret_cast<const u32x4_t*>(W.marks)[at];
+  if (RELEASE) m = reinterpret_cast<const u32x4_t*>(W.marks2)[at] & ~m;
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = m[i] & 0x01010101u;  // bytes 0 or 1 to bits 0 .. 3
+    bits |= ((v | v >> 7 | v >> 14 | v >> 21) & 15u) << (4 * i);
+  }
+  return bits;
+}
+
+template <bool RELEASE>
+__global__ __launch_bounds__(kThreads) void count_kernel(Pool W) {
+  __shared__ uint32_t waves[kThreads / 64];
+  uint32_t total;
+  block_scan<kThreads>(__popc(marks16<RELEASE>(W, blockIdx.x)), waves, total);
+  if (threadIdx.x == 0) W.counts[blockIdx.x] = (int)total;
+}
+
+// Counts of the blocks in front of `block`, and of all.
+__device__ __forceinline__ void blocks_before(const Pool& W, int block, uint32_t* waves, uint32_t& before, uint32_t& all) {
+  uint32_t a = 0, b = 0;
+  for (int i = threadIdx.x; i < W.blocks; i += kThreads) {
+    const uint32_t c = (uint32_t)W.counts[i];
+    b += c;
+    if (i < block) a += c;
+  }
+  block_scan<kThreads>(a, waves, before);
+  block_scan<kThreads>(b, waves, all);
+}
+
+__global__ __launch_bounds__(kThreads) void release_write_kernel(PageReleaseArgs A, Pool W) {
+  __shared__ uint32_t waves[kThreads / 64];
+  uint32_t before, all, mine;
+  blocks_before(W, blockIdx.x, waves, before, all);
+  uint32_t bits = marks16<true>(W, blockIdx.x);
+  const int first = W.header->a;
+  int at = first + (int)(before + block_scan<kThreads>(__popc(bits), waves, mine));
+  const int page0 = blockIdx.x * kBlockPages + threadIdx.x * 16;
+  for (; bits; bits &= bits - 1, ++at)
+    if (at < A.out_capacity) A.free_out[at] = page0 + __builtin_ctz(bits);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *A.n_free_out = min(first + (int)all, A.out_capacity);
+}
+
+// ---- compact
+
+struct Plan {
+  int used, low, moves;  // pages in use, those of them below `used`, moves
+  __device__ int holes() const { return used - low; }  // unused pages below `used`, as many as used ones above
+};
+
+// What page p is for the plan, c used pages in front of it.
+__device__ __forceinline__ void plan_page(const PageCompactArgs& A, const Plan& P, int p, bool used, int c) {
+  const int left = P.holes() - P.moves;  // unused pages below and used pages above that stay
+  if (p < P.used) {
+    if (used) return;
+    const int r = p - c;
+    if (r < P.moves) A.dst[r] = p;
+    else if (r - P.moves < A.free_capacity) A.free_pages[r - P.moves] = p;
+    return;
+  }
+  const int r = P.used - 1 - c;  // used pages above p
+  if (used && r >= P.moves) return;
+  if (used) A.src[r] = p;
+  const int at = left + (p - P.used) - min(c - P.low, left);
+  if (at < A.free_capacity) A.free_pages[at] = p;
+}
+
+__global__ __launch_bounds__(kThreads) void compact_mark_kernel(PageCompactArgs A, Pool W, int turns) {
+  for (int x = blockIdx.x; x < turns; x += gridDim.x)
+    for_held(A.table, A.seq_lens, A.max_pages, A.log2_page, A.n_pages, x, [&](int p) { W.marks[p] = 1; });
+}
+
+__global__ __launch_bounds__(kThreads) void compact_plan_kernel(PageCompactArgs A, Pool W) {
+  __shared__ uint32_t waves[kThreads / 64];
+  uint32_t before, all, low, x;
+  blocks_before(W, blockIdx.x, waves, before, all);
+  const int border = (int)all / kBlockPages;  // the block in which the pages below `used` end
+  if (border < W.blocks) {
+    blocks_before(W, border, waves, low, x);
+    const int n = (int)all - border * kBlockPages - (int)threadIdx.x * 16;  // this thread's pages below it
+    const uint32_t bits = marks16<false>(W, border) & (n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1u);
+    block_scan<kThreads>(__popc(bits), waves, x);
+    low += x;
+  } else {
+    low = all;
+  }
+  const Plan P{(int)all, (int)low, min((int)(all - low), A.max_moves)};
+  const uint32_t bits = marks16<false>(W, blockIdx.x);
+  int c = (int)(before + block_scan<kThreads>(__popc(bits), waves, x));
+  const int page0 = blockIdx.x * kBlockPages + threadIdx.x * 16;
+  for (int i = 0; i < 16; ++i) {
+    const bool used = bits >> i & 1;
+    if (page0 + i < A.n_pages) {
+      if (used && page0 + i >= P.used) W.ranks[page0 + i] = P.used - 1 - c;
+      plan_page(A, P, page0 + i, used, c);
+    }
+    c += used;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *A.n_moves = P.moves;
+    *A.n_free = (int)std::min(A.n_pages - P.used, (long long)A.free_capacity);
+    *W.header = Header{P.used, P.moves};
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void compact_table_kernel(PageCompactArgs A, Pool W, int turns) {
+  const Header H = *W.header;
+  const int per_row = (A.max_pages + kEntries - 1) / kEntries;
+  for (int x = blockIdx.x; x < turns; x += gridDim.x) {
+    const int row = x / per_row, j0 = x % per_row * kEntries, held = held_pages(A.seq_lens[row], A.max_pages, A.log2_page);
+    for (int j = j0 + threadIdx.x; j < min(j0 + kEntries, A.max_pages); j += kThreads) {
+      const size_t at = (size_t)row * A.max_pages + j;
+      int p = A.table[at];
+      if (j < held && p >= H.a && p < A.n_pages) {
+        const int r = W.ranks[p];
+        if (r < H.b) p = A.dst[r];
+      }
+      A.new_table[at] = p;
+    }
+  }
+}
+
+// ---- one workgroup
+
+constexpr int kOneThreads = 1024;
+constexpr int kOneWords = 4096;                // words of marks in LDS
+constexpr long long kOnePages = kOneWords * 32;
+
+template <class F>
+__device__ __forceinline__ void one_for_held(const int32_t* table, const int32_t* lens, int batch, int max_pages, int log2_page,
+                                             long long n_pages, F&& f) {
+  const int lane = threadIdx.x & 63;
+  for (int row = threadIdx.x >> 6; row < batch; row += kOneThreads / 64) {
+    const int held = held_pages(lens[row], max_pages, log2_page);
+    for (int j = lane; j < held; j += 64) {
+      const int p = table[(size_t)row * max_pages + j];
+      if (p >= 0 && p < n_pages) f(p);
+    }
+  }
+}
+
+__global__ __launch_bounds__(kOneThreads) void release_one_kernel(PageReleaseArgs A) {
+  __shared__ uint32_t now[kOneWords], before[kOneWords], waves[kOneThreads / 64];
+  const int words = (int)((A.n_pages + 31) / 32);
+  for (int i = threadIdx.x; i < words; i += kOneThreads) now[i] = before[i] = 0u;
+  int taken, n_free;
+  free_list(A, taken, n_free);
+  __syncthreads();
+  one_for_held(A.old_table, A.old_lens, A.old_batch, A.max_pages, A.log2_page, A.n_pages,
+               [&](int p) { atomicOr(&before[p >> 5], 1u << (p & 31)); });
+  one_for_held(A.new_table, A.new_lens, A.new_batch, A.max_pages, A.log2_page, A.n_pages,
+               [&](int p) { atomicOr(&now[p >> 5], 1u << (p & 31)); });
+  for (int i = taken + (int)threadIdx.x; i < n_free; i += kOneThreads) {
+    const int p = A.free_pages[i];
+    if (p >= 0 && p < A.n_pages) atomicOr(&now[p >> 5], 1u << (p & 31));
+    if (i - taken < A.out_capacity) A.free_out[i - taken] = p;
+  }
+  __syncthreads();
+  const int per = (words + kOneThreads - 1) / kOneThreads, w0 = min((int)threadIdx.x * per, words), w1 = min(w0 + per, words);
+  uint32_t mine = 0, total;
+  for (int w = w0; w < w1; ++w) mine += __popc(before[w] & ~now[w]);
+  int at = n_free - taken + (int)block_scan<kOneThreads>(mine, waves, total);
+  for (int w = w0; w < w1; ++w)
+    for (uint32_t bits = before[w] & ~now[w]; bits; bits &= bits - 1, ++at)
+      if (at < A.out_capacity) A.free_out[at] = w * 32 + __builtin_ctz(bits);
+  if (threadIdx.x == 0) *A.n_free_out = min(n_free - taken + (int)total, A.out_capacity);
+}
+
+__global__ __launch_bounds__(kOneThreads) void compact_one_kernel(PageCompactArgs A) {
+  __shared__ uint32_t marks[kOneWords], start[kOneWords], waves[kOneThreads / 64];  // start: used pages in front of a word
+  const int words = (int)((A.n_pages + 31) / 32);
+  for (int i = threadIdx.x; i < words; i += kOneThreads) marks[i] = 0u;
+  __syncthreads();
+  one_for_held(A.table, A.seq_lens, A.batch, A.max_pages, A.log2_page, A.n_pages,
+               [&](int p) { atomicOr(&marks[p >> 5], 1u << (p & 31)); });
+  __syncthreads();
+  const int per = (words + kOneThreads - 1) / kOneThreads, w0 = min((int)threadIdx.x * per, words), w1 = min(w0 + per, words);
+  uint32_t mine = 0, total;
+  for (int w = w0; w < w1; ++w) mine += __popc(marks[w]);
+  uint32_t at = block_scan<kOneThreads>(mine, waves, total);
+  for (int w = w0; w < w1; ++w) {
+    start[w] = at;
+    at += __popc(marks[w]);
+  }
+  __syncthreads();
+  const auto used_before = [&](int p) {
+    return (int)(start[p >> 5] + __popc(marks[p >> 5] & ((1u << (p & 31)) - 1u)));
+  };
+  const int low = (int)total < A.n_pages ? used_before((int)total) : (int)total;
+  const Plan P{(int)total, low, min((int)total - low, A.max_moves)};
+  for (int p = threadIdx.x; p < A.n_pages; p += kOneThreads)
+    plan_page(A, P, p, marks[p >> 5] >> (p & 31) & 1, used_before(p));
+  if (threadIdx.x == 0) {
+    *A.n_moves = P.moves;
+    *A.n_free = (int)std::min(A.n_pages - P.used, (long long)A.free_capacity);
+  }
+  __syncthreads();  // the moves are written
+  const int lane = threadIdx.x & 63;
+  for (int row = threadIdx.x >> 6; row < A.batch; row += kOneThreads / 64) {
+    const int held = held_pages(A.seq_lens[row], A.max_pages, A.log2_page);
+    for (int j = lane; j < A.max_pages; j += 64) {
+      const size_t e = (size_t)row * A.max_pages + j;
+      int p = A.table[e];
+      if (j < held && p >= P.used && p < A.n_pages) {
+        const int r = P.used - 1 - used_before(p);
+        if (r < P.moves) p = A.dst[r];
+      }
+      A.new_table[e] = p;
+    }
+  }
+}
+
+int turns_of(long long rows, int max_pages) { return (int)(rows * ((max_pages + kEntries - 1) / kEntries)); }
+int grid_of(long long n, int most) { return (int)std::min<long long>(std::max<long long>(n, 1), most); }
+
+void clear(void* p, size_t bytes, hipStream_t stream) {
+  const size_t n = bytes / 16;
+  hipLaunchKernelGGL(clear_kernel, dim3(grid_of((long long)((n + kThreads - 1) / kThreads), 1024)), dim3(kThreads), 0, stream,
+                     static_cast<u32x4_t*>(p), n);
+}
+
+// One workgroup where the tables' entries are few.
+constexpr long long kOneEntries = 1 << 16;
+
+}  // namespace
+
+size_t page_workspace_bytes(long long n_pages) { return Pool(nullptr, n_pages).bytes; }
+
+hipError_t launch_page_release(const PageReleaseArgs& a, hipStream_t stream) {
+  if (a.n_pages <= kOnePages && ((long long)a.old_batch + a.new_batch) * a.max_pages + a.free_capacity <= kOneEntries) {
+    hipLaunchKernelGGL(release_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  const Pool W(a.workspace, a.n_pages);
+  clear(W.marks, 2 * (size_t)W.blocks * kBlockPages, stream);
+  const int old_turns = turns_of(a.old_batch, a.max_pages), new_turns = turns_of(a.new_batch, a.max_pages);
+  const long long lists = ((long long)a.free_capacity + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL(release_mark_kernel, dim3(grid_of(std::max<long long>((long long)old_turns + new_turns, lists), 2048)),
+                     dim3(kThreads), 0, stream, a, W, old_turns, new_turns);
+  hipLaunchKernelGGL((count_kernel<true>), dim3(W.blocks), dim3(kThreads), 0, stream, W);
+  hipLaunchKernelGGL(release_write_kernel, dim3(W.blocks), dim3(kThreads), 0, stream, a, W);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_compact(const PageCompactArgs& a, hipStream_t stream) {
+  if (a.n_pages <= kOnePages && (long long)a.batch * a.max_pages <= kOneEntries) {
+    hipLaunchKernelGGL(compact_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  const Pool W(a.workspace, a.n_pages);
+  clear(W.marks, (size_t)W.blocks * kBlockPages, stream);
+  const int turns = turns_of(a.batch, a.max_pages);
+  hipLaunchKernelGGL(compact_mark_kernel, dim3(grid_of(turns, 2048)), dim3(kThreads), 0, stream, a, W, turns);
+  hipLaunchKernelGGL((count_kernel<false>), dim3(W.blocks), dim3(kThreads), 0, stream, W);
+  hipLaunchKernelGGL(compact_plan_kernel, dim3(W.blocks), dim3(kThreads), 0, stream, a, W);
+  hipLaunchKernelGGL(compact_table_kernel, dim3(grid_of(turns, 2048)), dim3(kThreads), 0, stream, a, W, turns);
+  return hipGetLastError();
+}
+
+}  // namespace cosa
