@@ -28,7 +28,7 @@ constexpr int kWaves = 8, kThreads = kWaves * 64;
 constexpr int kTile = kChunkTile;
 constexpr int kKeyTiles = kTile / 32;
 constexpr int kTileBytes = kTile * kHeadDim * 2;  // one tensor's
-constexpr int kGrid = 256;                        // workgroups that share the line: one a CU
+constexpr int kLog2Grid = 8, kGrid = 1 << kLog2Grid;  // workgroups that share the line: one a CU
 constexpr int kShortest = 256;                    // slots of the shortest range
 constexpr int kRowFloats = kHeadDim + 2;          // of a partial result: O, maximum, sum
 
@@ -41,7 +41,7 @@ struct ChunkParams {
   uint16_t* o;
   float* lse;
   int B, Hq, Hkv, G, GP, parts, T;  // GP: heads of a unit
-  int max_pages, log2_page, n_rows, part_rows, grid;
+  int max_pages, log2_page, n_rows, part_rows, log2_grid;
   long long q_stride, n_pages;
   float scale, scale_log2;
 };
@@ -65,23 +65,33 @@ __device__ __forceinline__ ChunkSeq seq_of(const ChunkParams& P, int n) {
 __device__ __forceinline__ int32_t ld_uniform(const int32_t* p) {
   return *(const __attribute__((address_space(4))) int32_t*)(size_t)p;
 }
-__device__ __forceinline__ ChunkSeq seq_of_uniform(const ChunkParams& P, int n, int& row0) {
-  return seq_of(P, ld_uniform(P.cu_new + n), ld_uniform(P.cu_new + n + 1), ld_uniform(P.seq_lens + n), row0);
-}
 // Values that are the same in every lane, in scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
 }
 
-// Heads of unit part hp of a group, its first head, and the rows of unit j.
+__device__ __forceinline__ ChunkSeq seq_of_uniform(const ChunkParams& P, int n, int& row0) {
+  const ChunkSeq S = seq_of(P, ld_uniform(P.cu_new + n), ld_uniform(P.cu_new + n + 1), ld_uniform(P.seq_lens + n), row0);
+  row0 = uniform(row0);
+  return {uniform(S.len), uniform(S.w), P.T};
+}
+
+// Heads of unit part hp of a group.
 __device__ __forceinline__ int heads_of(const ChunkParams& P, int hp) { return min(P.G - hp * P.GP, P.GP); }
 
-__device__ __forceinline__ void store8(uint16_t* to, const float (&x)[4], float by) {
+// A value that is formed again where it is used, not held in a register over the walk.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Four results as bf16.
+__device__ __forceinline__ void store4(uint16_t* to, const float (&x)[4]) {
   uint32_t w[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const __bf16 lo = (__bf16)(x[2 * e] * by), hi = (__bf16)(x[2 * e + 1] * by);
+    const __bf16 lo = (__bf16)x[2 * e], hi = (__bf16)x[2 * e + 1];
     w[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
   }
   *reinterpret_cast<u32x2_t*>(to) = u32x2_t{w[0], w[1]};
@@ -99,81 +109,244 @@ __device__ __forceinline__ void end_phase(bool full) {
 struct Lds {
   char v[2][kTileBytes];  // the low 64 KiB: every transposing read's offsets fit its immediate
   char k[2][kTileBytes];
+  int32_t unit[kWaves][2][16];  // a wave's unit and its next one
+  int64_t range[3];             // the range's first slot and its end, and the length of all ranges
+  int odd[2][4];  // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
 };
 
-// Tiles [t0, t1) of unit j of sequence n; the result goes to o and lse (part == nullptr) or to part.
-__device__ __forceinline__ void walk(const ChunkParams& P, Lds& lds, const ChunkSeq& S, int n, int row0, int g, int hp, int j,
-                                     int t0, int t1, float* part) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int side = w >> 2, wl = w & 3;  // waves w and w + 4 share a SIMD; side 1 runs one phase behind
-  const int heads = heads_of(P, hp);
-  const int first = j * P.T;  // first token
-  const int rows = uniform(min(P.T, S.w - first) * heads);
-  const int keys = uniform(S.keys(j));
-
-  // This lane's row (behind the unit's last one: that one again, which is not stored).
-  const int xr = min(w * 32 + l32, rows - 1), tok = xr / heads;
-  const int row = row0 + first + tok, h = g * P.G + hp * P.GP + (xr - tok * heads);
-  const int pos = S.len - S.w + first + tok;
-  const int pos_low = __builtin_amdgcn_readfirstlane(pos);                                  // of the wave's rows
-  const int pos_top = __builtin_amdgcn_readlane(pos, 31);
-  const bool live = w * 32 < rows;
-
-  bf16x8_t qf[8];
-  {
-    const uint16_t* qp = P.q + (size_t)row * P.q_stride + (size_t)h * kHeadDim + 8 * half;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) qf[c] = as_bf16x8(ldg16(qp + 16 * c));
+// A unit of the line and the range's tiles of it.
+struct Unit {
+  ChunkSeq S;
+  int n, row0;  // sequence, its first row
+  int hh, j;    // KV head and part, unit of these
+  int64_t at;   // its first slot
+  int tiles, t0, t1;
+};
+// Units wait in LDS, one copy a wave: in scalar registers, two of them would push other values out.
+__device__ __forceinline__ void put(int32_t* to, const Unit& u) {
+  if ((threadIdx.x & 63) == 0) {
+    int4* p = reinterpret_cast<int4*>(to);
+    p[0] = int4{u.S.len, u.S.w, u.n, u.row0};
+    p[1] = int4{u.hh, u.j, (int)u.at, (int)(u.at >> 32)};
+    p[2] = int4{u.tiles, u.t0, u.t1, 0};
   }
+}
+__device__ __forceinline__ Unit get(const int32_t* from, int T) {
+  asm volatile("" ::: "memory");
+  const int4* p = reinterpret_cast<const int4*>(from);
+  const int4 a = p[0], b = p[1], c = p[2];
+  return {{uniform(a.x), uniform(a.y), T}, uniform(a.z), uniform(a.w), uniform(b.x), uniform(b.y),
+          (int64_t)(uint32_t)uniform(b.z) | (int64_t)uniform(b.w) << 32, uniform(c.x), uniform(c.y), uniform(c.z)};
+}
 
-  // Copies. Side 0 moves K, side 1 V: wave wl rows 32 wl .. 32 wl + 31 of a tile, in two runs of 16. A lane fills slot
-  // lane % 16 of row lane / 16 of four rows with the slot that the layout puts there (K: slot ^ row % 16, V: slot ^ 4 (row %
-  // 4), as the MFMA operand and the transposing reads want them).
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads))) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void chunk_kernel(const ChunkParams P) {
+  __shared__ __attribute__((aligned(1024))) Lds lds;
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int w = uniform((int)threadIdx.x >> 6);
+
+  // The range of this workgroup, and its first unit. Slots of the sequences: one a lane, every wave for itself, or a
+  // stretch of them a thread.
+  const int all_heads = P.Hkv * P.parts;
+  Unit D;
+  int64_t begin, end, total = 0;
+  int b;
+  const auto place = [&]() __attribute__((always_inline)) {
+    const int64_t length = chunk_range(total, P.log2_grid, kShortest);
+    // Neighbouring ranges, which mostly share a KV head, go to one XCD: of all ranges, or of those with slots.
+    const int per_xcd = length > kShortest ? gridDim.x / kNumXcd : (int)((total + kShortest * kNumXcd - 1) / (kShortest * kNumXcd));
+    const int k = blockIdx.x / kNumXcd;
+    b = k < per_xcd ? (blockIdx.x % kNumXcd) * per_xcd + k : (int)blockIdx.x;
+    begin = k < per_xcd ? b * length : total;
+    end = min(begin + length, total);
+    if (threadIdx.x == 0) lds.range[2] = length;
+  };
+  const auto of = [&](int64_t x, int l) __attribute__((always_inline)) -> int64_t {
+    return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, l) | (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32;
+  };
+  const auto scan = [&](int64_t x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up((long long)x, d, 64);
+      if (lane >= d) x += y;
+    }
+    return x;
+  };
+  if (P.B <= 64) {
+    int row0 = 0;
+    ChunkSeq S{0, 0, P.T};
+    if (lane < P.B) S = seq_of(P, P.cu_new[lane], P.cu_new[lane + 1], P.seq_lens[lane], row0);
+    const int64_t mine = S.slots() * all_heads;
+    const int64_t at = P.B == 1 ? mine : scan(mine);
+    total = of(at, P.B - 1);
+    place();
+    if (begin < total) {
+      D.n = __builtin_popcountll(__ballot(lane < P.B && at <= begin));  // the sequences that end in front of it
+      D.at = of(at - mine, D.n);
+      D.S = ChunkSeq{__builtin_amdgcn_readlane(S.len, D.n), __builtin_amdgcn_readlane(S.w, D.n), P.T};
+      D.row0 = __builtin_amdgcn_readlane(row0, D.n);
+    }
+  } else {
+    __shared__ int64_t sums[kWaves];
+    __shared__ int64_t found_at;
+    __shared__ int found;
+    const int per = (P.B + kThreads - 1) / kThreads;
+    const int n0 = min((int)threadIdx.x * per, P.B), n1 = min(n0 + per, P.B);
+    int64_t mine = 0;
+    for (int n = n0; n < n1; ++n) mine += seq_of(P, n).slots() * all_heads;
+    int64_t at = scan(mine);
+    if (lane == 63) sums[w] = at;
+    __syncthreads();
+    at -= mine;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      if (i < w) at += sums[i];
+      total += sums[i];
+    }
+    total = uniform(total);
+    place();
+    if (begin < total) {
+      if (begin >= at && begin < at + mine) {
+        int n = n0;
+        for (;; ++n) {
+          const int64_t t = seq_of(P, n).slots() * all_heads;
+          if (begin < at + t) break;
+          at += t;
+        }
+        found = n;
+        found_at = at;
+      }
+      __syncthreads();
+      D.n = uniform(found);
+      D.at = uniform(found_at);
+      D.S = seq_of_uniform(P, D.n, D.row0);
+    }
+  }
+  if (threadIdx.x == 0) P.rec[b] = int4{-1, 0, 0, 0};
+  if (begin >= total) return;
+  {
+    // largest i in [0, n) with start(i) <= x
+    const auto search = [&](int n, int64_t x, auto&& start) __attribute__((always_inline)) -> int {
+      int first = 0;
+      for (int step = search_step(n); step; step /= 64) {
+        const int64_t i = (int64_t)first + (int64_t)lane * step;
+        first += (__builtin_popcountll(__ballot(i < n && start((int)i) <= x)) - 1) * step;
+      }
+      return first;
+    };
+    const int64_t one = uniform(D.S.slots());
+    D.hh = search(all_heads, begin - D.at, [&](int i) { return one * i; });
+    D.at += D.hh * one;
+    D.j = search(D.S.units(), begin - D.at, [&](int i) { return D.S.start(i); });
+    D.at = uniform(D.at + D.S.start(D.j));
+  }
+  const auto settle = [&](Unit& u, int64_t begin, int64_t end) __attribute__((always_inline)) {
+    u.tiles = uniform(u.S.tiles(u.j));
+    u.t0 = uniform(chunk_tile0(begin, u.at));
+    u.t1 = uniform(chunk_tile1(end, u.at, u.tiles));
+  };
+  // The next unit of the range (its first one may have no tile here).
+  const auto advance = [&](Unit& u, int64_t begin, int64_t end) __attribute__((always_inline)) -> bool {
+    u.at = uniform(u.at + u.S.keys(u.j) + kUnitSlots);
+    if (u.at >= end) return false;
+    if (++u.j == u.S.units()) {
+      u.j = 0;
+      if (++u.hh == all_heads) {
+        u.hh = 0;
+        do u.S = seq_of_uniform(P, ++u.n, u.row0); while (u.S.w == 0);  // there are slots left, so there is one
+      }
+    }
+    settle(u, begin, end);
+    return true;
+  };
+  settle(D, begin, end);
+  if (threadIdx.x == 0) {
+    lds.range[0] = begin;
+    lds.range[1] = end;
+  }
+  if (D.t0 >= D.t1 && !advance(D, begin, end)) return;
+
+  // Copies. Waves w and w + 4 share a SIMD; side 1 (w >= 4) runs one phase behind. Side 0 moves K, side 1 V: wave wl rows 32
+  // wl .. 32 wl + 31 of a tile, in two runs of 16. A lane fills slot lane % 16 of row lane / 16 of four rows with the
+  // slot that the layout puts there (K: slot ^ row % 16, V: slot ^ 4 (row % 4), as the MFMA operand and the transposing
+  // reads want them).
+  const int side = w >> 2, wl = w & 3;
   const uint64_t head_bytes = (uint64_t)(kHeadDim * 2) << P.log2_page;
   const uint64_t page_bytes = head_bytes * (uint64_t)P.Hkv;
-  const uint64_t cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)g * head_bytes));
   const int page_mask = (1 << P.log2_page) - 1;
-  const int32_t* trow = P.table + (size_t)n * P.max_pages;
-  const int vk = (lane >> 4) * 256 + (((lane & 15) ^ (lane >> 4)) << 4);
-  const int vv = (lane >> 4) * 256 + (((lane & 15) ^ ((lane >> 4) << 2)) << 4);
+  const int lane_off = (lane >> 4) * 256 + (((lane & 15) ^ (side ? (lane >> 4) << 2 : lane >> 4)) << 4);
+  const int step_off = side ? 0 : 64;  // K: slots of rows 4 further on differ in two more bits
+  // The unit whose tiles are fetched: its keys, its KV head's cache, and its first token's place.
+  int f_keys, f_first;
+  uint64_t f_cache;
+  const int32_t* f_row;
   int pg[2];
+  const auto fetch_from = [&](const Unit& u) __attribute__((always_inline)) {
+    f_keys = uniform(u.S.keys(u.j));
+    f_first = u.S.len - u.S.w + u.j * P.T;
+    f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)(u.hh / P.parts) * head_bytes));
+    f_row = P.table + (size_t)u.n * P.max_pages;
+  };
   // Physical pages of the runs of tiles t .. t + 63, one tile a lane (run r: rows 32 wl + 16 r).
-  auto look_up = [&](int t) __attribute__((always_inline)) {
+  const auto look_up = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int64_t at = (int64_t)(t + lane) * kTile + wl * 32 + r * 16;
+      const int64_t x = (int64_t)(t + lane) * kTile + wl * 32 + r * 16;
       int p = 0;
-      if (at < keys) p = trow[at >> P.log2_page];
-      pg[r] = (uint32_t)p < (uint64_t)P.n_pages ? p : 0;
+      if (x < f_keys) p = f_row[x >> P.log2_page];
+      pg[r] = p;
     }
   };
-  auto copy = [&](auto is_k, int t, int i, char* dst) __attribute__((always_inline)) {
-    constexpr bool IS_K = decltype(is_k)::value;
+  const auto copy = [&](int t, int i, int buf) __attribute__((always_inline)) {
+    char* dst = (side ? lds.v[0] : lds.k[0]) + buf * kTileBytes + wl * 32 * 256;
+    const int off = again(lane_off);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int at = t * kTile + wl * 32 + r * 16;  // below 2^31 + 128 where it holds a key
-      const int valid = uniform(min(max(keys - at, 0), 16));
-      const uint64_t p = (uint32_t)__builtin_amdgcn_readlane(pg[r], i & 63);
-      const uint64_t base = cache + p * page_bytes + (uint64_t)(at & page_mask) * (kHeadDim * 2);
+      const int x = t * kTile + wl * 32 + r * 16;  // below 2^31 + 128 where it holds a key
+      const int valid = uniform(min(max(f_keys - x, 0), 16));
+      const uint32_t e = (uint32_t)__builtin_amdgcn_readlane(pg[r], i & 63);
+      const uint64_t p = e < (uint64_t)P.n_pages ? e : 0u;
+      const uint64_t base = f_cache + p * page_bytes + (uint64_t)(x & page_mask) * (kHeadDim * 2);
       const __amdgpu_buffer_rsrc_t rs =
           __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, valid * (kHeadDim * 2), 0x00020000);
-      const auto to = COSA_LDS(dst + (wl * 32 + r * 16) * 256);
+      const auto to = COSA_LDS(dst + r * 16 * 256);
       // the immediate offset counts for the bounds and moves both addresses
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, IS_K ? vk : vv, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, IS_K ? vk ^ 64 : vv, 0, 1024, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, IS_K ? vk ^ 128 : vv, 0, 2048, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, IS_K ? vk ^ 192 : vv, 0, 3072, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, off ^ step_off, 0, 1024, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, off ^ (2 * step_off), 0, 2048, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, off ^ (3 * step_off), 0, 3072, 0);
     }
   };
-
-  f32x16_t o[4];
+  // Side 1, once its part of V tile t has landed, where some row does not see the whole tile: infinite and NaN values would
+  // give NaN with that row's weights of 0. They become 0, and the end of the unit adds them to the rows that see them.
+  const auto clean = [&](int t, int buf) __attribute__((always_inline)) {
+    if (side == 0 || f_first - t * kTile >= kTile - 1) return;
+    __builtin_amdgcn_s_waitcnt(kVmcntLgkm0);
+    asm volatile("" ::: "memory");
+    float sum = 0.f;
+    char* part = lds.v[0] + buf * kTileBytes + wl * 32 * 256 + again(lane) * 16;
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
+    for (int i = 0; i < 8; ++i) {
+      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(part + i * 1024);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m = -INFINITY;  // running maximum of the raw logits, the same in both halves
-  float lsum = 0.f;     // this half's share of the sum
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t two = v[e];
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, two), bf16x2_t{(__bf16)0.f, (__bf16)0.f}, sum, false);
+      }
+    }
+    const int any = __any(sum != 0.f);
+    if (lane == 0) lds.odd[buf][wl] = any;
+    if (any) {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        u32x4_t v = *reinterpret_cast<const u32x4_t*>(part + i * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] &= ((v[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((v[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+        *reinterpret_cast<u32x4_t*>(part + i * 1024) = v;
+      }
+    }
+  };
 
   // LDS read offsets. K: key 32 t + l32, slot 2 c + half: k_rd ^ 32 c. V: transposing reads of rows 32 t + 16 c2 + 8 a +
   // 4 half + i / 4 and columns 32 dt + 16 g16 + 4 (i % 4), with i = lane % 16 and g16 = (lane / 16) % 2: v_rd ^ 64 dt.
@@ -182,337 +355,317 @@ __device__ __forceinline__ void walk(const ChunkParams& P, Lds& lds, const Chunk
   const int v_rd = (4 * half + (li >> 2)) * 256 + (((2 * ((lane >> 4) & 1) + ((li & 3) >> 1)) ^ ((li >> 2) << 2)) << 4) +
                    8 * (li & 1);
 
-  // First key of the rest that finish() takes: from the first tile on that holds an infinite or NaN value which some
-  // row does not see, where 0 times it would be NaN.
-  int rest = INT_MAX;
-  // What QK hands to PV of the same tile.
-  struct Logits {
-    f32x16_t s[kKeyTiles];
-    float mnew;
-    bool on;    // the wave sees something of the tile
-    bool edge;  // and some of its rows not all of it
-    int key0;
+  // This lane's row of unit u: token and head (behind the unit's last token: that one again, which is not stored).
+  const auto row_of = [&](const Unit& u, int x, int& tok, int& head) __attribute__((always_inline)) -> int {
+    const int hp = uniform(u.hh % P.parts), heads = heads_of(P, hp), tokens = min(P.T, u.S.w - u.j * P.T);
+    tok = x / heads;
+    head = uniform(u.hh / P.parts) * P.G + hp * P.GP + (x - tok * heads);
+    const bool real = tok < tokens;
+    tok = u.j * P.T + min(tok, tokens - 1);
+    return real;
   };
-  auto qk_half = [&](int t, auto bufc, Logits& X) __attribute__((always_inline)) {
-    const char* Kb = lds.k[decltype(bufc)::value];
-    const int key0 = t * kTile;
-    auto& s = X.s;
-    X.key0 = key0;
-    X.on = live && key0 <= pos_top && rest == INT_MAX;
-    X.edge = pos_low - key0 < kTile - 1;
-    if (!X.on) return;
+  bf16x8_t qf[8];
+  int pos;  // of the lane's row
+  const auto load_q = [&](const Unit& u) __attribute__((always_inline)) {
+    int tok, head;
+    const int ln = again(lane);
+    row_of(u, w * 32 + (ln & 31), tok, head);
+    pos = u.S.len - u.S.w + tok;
+    const uint16_t* qp = P.q + (size_t)(u.row0 + tok) * P.q_stride + (size_t)head * kHeadDim + 8 * (ln >> 5);
 #pragma unroll
-    for (int tt = 0; tt < kKeyTiles; ++tt)
+    for (int c = 0; c < 8; ++c) qf[c] = as_bf16x8(ldg16(qp + 16 * c));
+  };
+
+  int buf = 0;
+  fetch_from(D);
+  look_up(D.t0);
+  load_q(D);
+  copy(D.t0, 0, 0);
+  clean(D.t0, 0);
+  end_phase(true);
+  if (side == 1) end_phase(false);
+
+  int parity = 0;
+  put(lds.unit[w][0], D);
+  for (;;) {
+    const Unit D = get(lds.unit[w][parity], P.T);
+    const bool live = w * 32 < min(P.T, D.S.w - D.j * P.T) * heads_of(P, uniform(D.hh % P.parts));
+    const int pos_low = uniform(pos);  // of the wave's rows
+    const int pos_top = __builtin_amdgcn_readlane(pos, 31);
+    f32x16_t o[4];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[tt][r] = 0.f;
-    int kr = k_rd;
-    asm volatile("" : "+v"(kr));  // the chunks' offsets are formed here, not held in registers
-    bf16x8_t kf[2][kKeyTiles];
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int tt = 0; tt < kKeyTiles; ++tt)
-      kf[0][tt] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Kb + kr + tt * 32 * 256));
-    __builtin_amdgcn_sched_group_barrier(0x100, kKeyTiles, 0);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      if (c + 1 < 8) {
-#pragma unroll
-        for (int tt = 0; tt < kKeyTiles; ++tt)
-          kf[(c + 1) & 1][tt] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Kb + (kr ^ (32 * (c + 1))) + tt * 32 * 256));
-      }
-#pragma unroll
-      for (int tt = 0; tt < kKeyTiles; ++tt) s[tt] = mfma32x32x16(kf[c & 1][tt], qf[c], s[tt]);
-      if (c + 1 < 8) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, kKeyTiles, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, kKeyTiles - 1, 0);
-      } else {
-        __builtin_amdgcn_sched_group_barrier(0x008, kKeyTiles, 0);
-      }
-    }
-    if (X.edge) {  // keys behind the row's token (and the zeros behind the last key): -inf, bit by bit
-      int qh = pos - key0 - 4 * half;
-      asm volatile("" : "+v"(qh));
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    float m = -INFINITY;  // running maximum of the raw logits, the same in both halves
+    float lsum = 0.f;     // this half's share of the sum
+    int odd_from = INT_MAX;  // first key of the first tile that was cleaned
+    const int first_pos = D.S.len - D.S.w + D.j * P.T;
+
+    // What QK hands to PV of the same tile.
+    struct Logits {
+      f32x16_t s[kKeyTiles];
+      float mnew;
+      bool on;    // the wave sees something of the tile
+      bool edge;  // and some of its rows not all of it
+    };
+    const auto qk_half = [&](int t, Logits& X) __attribute__((always_inline)) {
+      const int key0 = t * kTile;
+      auto& s = X.s;
+      X.on = live && key0 <= pos_top;
+      X.edge = pos_low - key0 < kTile - 1;
+      if (!X.on) return;
 #pragma unroll
       for (int tt = 0; tt < kKeyTiles; ++tt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          int d = qh - (32 * tt + 8 * (r >> 2) + (r & 3));
-          asm volatile("" : "+v"(d));
-          const uint32_t masked = (uint32_t)(d >> 31);
-          const float sv = s[tt][r];
-          const uint32_t bits = __builtin_bit_cast(uint32_t, sv);
-          s[tt][r] = __builtin_bit_cast(float, (bits & ~masked) | (0xFF800000u & masked));
-        }
-    }
-    float mloc = -INFINITY;
+        for (int r = 0; r < 16; ++r) s[tt][r] = 0.f;
+      int kr = k_rd;
+      asm volatile("" : "+v"(kr));  // the chunks' offsets are formed here, not held in registers
+      const char* Kb = lds.k[0] + buf * kTileBytes;
+      bf16x8_t kf[2][kKeyTiles];
 #pragma unroll
-    for (int tt = 0; tt < kKeyTiles; ++tt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mloc = fmaxf(mloc, s[tt][r]);
-    X.mnew = fmaxf(m, half_max(mloc));
-  };
-
-  auto odd_values = [&](const char* Vb) __attribute__((always_inline)) -> bool {
-    float sum = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < kTileBytes / 1024; ++i) {
-      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(Vb + i * 1024 + lane * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t two = v[e];
-        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, two), bf16x2_t{(__bf16)0.f, (__bf16)0.f}, sum, false);
-      }
-    }
-    return __any(sum != 0.f);
-  };
-  auto pv_half = [&](auto bufc, const Logits& X) __attribute__((always_inline)) {
-    if (!X.on) return;
-    const auto& s = X.s;
-    const float mnew = X.mnew;
-    const char* Vb = lds.v[decltype(bufc)::value];
-    if (X.edge && odd_values(Vb)) {
-      rest = X.key0;
-      return;
-    }
-    __builtin_amdgcn_s_setprio(1);
-    // Differences are taken before the scale: a scaled maximum's rounding would be a factor of every weight.
-    const float base = mnew == -INFINITY ? 0.f : mnew;
-    const float alpha = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
-    m = mnew;
-    if (__any(alpha != 1.f)) {
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
-    }
-    constexpr int KC = kTile / 16;
-    bf16x8_t pf[KC];
-    float rs = 0.f;
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float pv = __builtin_amdgcn_exp2f((s[kc >> 1][8 * (kc & 1) + e] - base) * P.scale_log2);
-        rs += pv;
-        pf[kc][e] = (__bf16)pv;
-      }
-    lsum = fmaf(lsum, alpha, rs);
-    const int v_at = (int)(size_t)COSA_LDS(Vb) + v_rd;
-    int va[4];
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) va[dt] = v_at ^ (64 * dt);
-    // Issued directly, so that the offsets go into the instruction; the wait names the fragments, which hands them to
-    // the MFMAs and keeps their registers reserved until the data has landed.
-    s16x4_t lo[2][4], hi[2][4];
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt) {
-      asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(lo[0][dt]) : "v"(va[dt]), "i"(0));
-      asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi[0][dt]) : "v"(va[dt]), "i"(8 * 256));
-    }
-#pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      const int b = kc & 1, nx = b ^ 1;
-      asm volatile("s_waitcnt lgkmcnt(0)"
-                   : "+v"(lo[b][0]), "+v"(lo[b][1]), "+v"(lo[b][2]), "+v"(lo[b][3]), "+v"(hi[b][0]), "+v"(hi[b][1]),
-                     "+v"(hi[b][2]), "+v"(hi[b][3]));
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        o[dt] = mfma32x32x16(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo[b][dt], hi[b][dt], 0, 1, 2, 3, 4, 5, 6, 7)),
-                             pf[kc], o[dt]);
-      if (kc + 1 < KC) {
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) {
-          asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(lo[nx][dt]) : "v"(va[dt]), "i"((kc + 1) * 16 * 256));
-          asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2"
-                       : "=v"(hi[nx][dt]) : "v"(va[dt]), "i"((kc + 1) * 16 * 256 + 8 * 256));
-        }
-      }
-      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);  // the chunk's MFMAs ...
-      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // ... then the next chunk's reads
-    }
-    __builtin_amdgcn_s_setprio(0);
-  };
-
-  constexpr std::integral_constant<int, 0> B0{};
-  constexpr std::integral_constant<int, 1> B1{};
-  int i = 0;  // tiles behind the last look_up
-  look_up(t0);
-  if (side == 0) copy(std::true_type{}, t0, 0, lds.k[0]);
-  else copy(std::false_type{}, t0, 0, lds.v[0]);
-  end_phase(true);
-
-  // Tile t in buffers BUF: QK, fetch tile t + 1 into the other buffers, barrier, PV, barrier. A wave waits for its own
-  // copies at the end of its PV half, a barrier before the other side or it itself reads them.
-  auto tile = [&](int t, auto bufc) __attribute__((always_inline)) {
-    constexpr int BUF = decltype(bufc)::value;
-    Logits X;
-    qk_half(t, bufc, X);
-    if (t + 1 < t1) {
-      if (++i == 64) {
-        look_up(t + 1);
-        i = 0;
-      }
-      if (side == 0) copy(std::true_type{}, t + 1, i, lds.k[BUF ^ 1]);
-      else copy(std::false_type{}, t + 1, i, lds.v[BUF ^ 1]);
-    }
-    end_phase(false);
-    pv_half(bufc, X);
-    end_phase(true);
-  };
-  if (side == 1) end_phase(false);
-  for (int t = t0; t < t1; t += 2) {
-    tile(t, B0);
-    if (t + 1 < t1) tile(t + 1, B1);
-  }
-  if (side == 0) end_phase(false);  // as many barriers on both sides
-
-  // The keys from `rest` on one by one, for values that only some rows see (at most the unit's last tiles).
-  const auto finish = [&]() __attribute__((always_inline)) {
-    const int to = (int)min((int64_t)t1 * kTile, (int64_t)pos_top + 1);
-#pragma unroll 1
-    for (int t = rest; t < to; ++t) {
-      const int32_t e = ld_uniform(trow + (t >> P.log2_page));
-      const uint64_t p = (uint32_t)e < (uint64_t)P.n_pages ? (uint32_t)e : 0u;
-      const size_t at = (p * page_bytes + (uint64_t)g * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim;
-      float dot = 0.f;
+      for (int tt = 0; tt < kKeyTiles; ++tt)
+        kf[0][tt] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Kb + kr + tt * 32 * 256));
+      __builtin_amdgcn_sched_group_barrier(0x100, kKeyTiles, 0);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const bf16x8_t k = as_bf16x8(ldg16(P.kc + at + 16 * c + 8 * half));
+        if (c + 1 < 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dot = fmaf((float)k[i], (float)qf[c][i], dot);
-      }
-      const bool sees = t <= pos;
-      dot = half_sum(dot);
-      const float logit = sees ? dot : -INFINITY;
-      const float mn = fmaxf(m, logit), base = mn == -INFINITY ? 0.f : mn;
-      const float alpha = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
-      const float pv = __builtin_amdgcn_exp2f((logit - base) * P.scale_log2);
-      m = mn;
-      lsum = lsum * alpha + (half == 0 ? pv : 0.f);
+          for (int tt = 0; tt < kKeyTiles; ++tt)
+            kf[(c + 1) & 1][tt] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(Kb + (kr ^ (32 * (c + 1))) + tt * 32 * 256));
+        }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const u32x2_t v = *reinterpret_cast<const u32x2_t*>(P.vc + at + 8 * i + 4 * half);
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          const float x = __uint_as_float(z & 1 ? v[z >> 1] & 0xffff0000u : v[z >> 1] << 16);
-          o[i >> 2][4 * (i & 3) + z] = o[i >> 2][4 * (i & 3) + z] * alpha + (sees ? pv * x : 0.f);
+        for (int tt = 0; tt < kKeyTiles; ++tt) s[tt] = mfma32x32x16(kf[c & 1][tt], qf[c], s[tt]);
+        if (c + 1 < 8) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, kKeyTiles, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, kKeyTiles - 1, 0);
+        } else {
+          __builtin_amdgcn_sched_group_barrier(0x008, kKeyTiles, 0);
         }
       }
+      if (X.edge) {  // keys behind the row's token (and the zeros behind the last key): -inf, bit by bit
+        int qh = pos - key0 - 4 * half;
+        asm volatile("" : "+v"(qh));
+#pragma unroll
+        for (int tt = 0; tt < kKeyTiles; ++tt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            int d = qh - (32 * tt + 8 * (r >> 2) + (r & 3));
+            asm volatile("" : "+v"(d));
+            const uint32_t masked = (uint32_t)(d >> 31);
+            const float sv = s[tt][r];
+            const uint32_t bits = __builtin_bit_cast(uint32_t, sv);
+            s[tt][r] = __builtin_bit_cast(float, (bits & ~masked) | (0xFF800000u & masked));
+          }
+      }
+      float mloc = -INFINITY;
+#pragma unroll
+      for (int tt = 0; tt < kKeyTiles; ++tt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mloc = fmaxf(mloc, s[tt][r]);
+      X.mnew = fmaxf(m, half_max(mloc));
+    };
+
+    const auto pv_half = [&](const Logits& X) __attribute__((always_inline)) {
+      if (!X.on) return;
+      const auto& s = X.s;
+      const float mnew = X.mnew;
+      __builtin_amdgcn_s_setprio(1);
+      // Differences are taken before the scale: a scaled maximum's rounding would be a factor of every weight.
+      const float base = mnew == -INFINITY ? 0.f : mnew;
+      const float alpha = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
+      m = mnew;
+      if (__any(alpha != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      }
+      constexpr int KC = kTile / 16;
+      bf16x8_t pf[KC];
+      float rs = 0.f;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float pv = __builtin_amdgcn_exp2f((s[kc >> 1][8 * (kc & 1) + e] - base) * P.scale_log2);
+          rs += pv;
+          pf[kc][e] = (__bf16)pv;
+        }
+      lsum = fmaf(lsum, alpha, rs);
+      const int v_at = (int)(size_t)COSA_LDS(lds.v[0]) + buf * kTileBytes + v_rd;
+      int va[4];
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) va[dt] = v_at ^ (64 * dt);
+      // Issued directly, so that the offsets go into the instruction; the wait names the fragments, which hands them to
+      // the MFMAs and keeps their registers reserved until the data has landed.
+      s16x4_t lo[2][4], hi[2][4];
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(lo[0][dt]) : "v"(va[dt]), "i"(0));
+        asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi[0][dt]) : "v"(va[dt]), "i"(8 * 256));
+      }
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        const int c = kc & 1, nx = c ^ 1;
+        asm volatile("s_waitcnt lgkmcnt(0)"
+                     : "+v"(lo[c][0]), "+v"(lo[c][1]), "+v"(lo[c][2]), "+v"(lo[c][3]), "+v"(hi[c][0]), "+v"(hi[c][1]),
+                       "+v"(hi[c][2]), "+v"(hi[c][3]));
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+          o[dt] = mfma32x32x16(
+              __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo[c][dt], hi[c][dt], 0, 1, 2, 3, 4, 5, 6, 7)), pf[kc], o[dt]);
+        if (kc + 1 < KC) {
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) {
+            asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(lo[nx][dt]) : "v"(va[dt]), "i"((kc + 1) * 16 * 256));
+            asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2"
+                         : "=v"(hi[nx][dt]) : "v"(va[dt]), "i"((kc + 1) * 16 * 256 + 8 * 256));
+          }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);  // the chunk's MFMAs ...
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // ... then the next chunk's reads
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+
+    // Tile t: QK, fetch the next tile (of this unit or of the next one) into the other buffers, barrier, PV, barrier. A
+    // wave waits for its own copies at the end of its PV half, a barrier before the other side or it itself reads them.
+    bool more = false;
+    int i = 0;  // tiles behind the last look_up
+    const int t1 = D.t1;
+    int t_end = t1;
+    asm volatile("" : "+s"(t_end));  // a loop of its own: `last` is not taken for its exit
+    for (int t = D.t0; t < t_end; ++t) {
+      const bool last = t + 1 == t1;
+      int to = t + 1;
+      if (last) {
+        Unit N = get(lds.unit[w][parity], P.T);
+        more = advance(N, uniform(lds.range[0]), uniform(lds.range[1]));
+        i = 0;
+        to = 0;
+        if (more) {
+          put(lds.unit[w][parity ^ 1], N);
+          fetch_from(N);
+          look_up(0);
+        }
+      } else if (++i == 64) {
+        look_up(to);
+        i = 0;
+      }
+      const bool fetch = !last || more;
+      Logits X;
+      qk_half(t, X);
+      if (last && more) load_q(get(lds.unit[w][parity ^ 1], P.T));  // its registers are free from here on
+      if (fetch) copy(to, i, buf ^ 1);
+      end_phase(false);
+      if (first_pos - t * kTile < kTile - 1) {
+        const u32x4_t odd = *reinterpret_cast<const u32x4_t*>(lds.odd[buf]);
+        if (uniform((int)(odd[0] | odd[1] | odd[2] | odd[3]))) odd_from = min(odd_from, t * kTile);
+      }
+      pv_half(X);
+      if (fetch) clean(to, buf ^ 1);
+      end_phase(true);
+      buf ^= 1;
     }
-  };
-  if (rest != INT_MAX) finish();
-  lsum = half_sum(lsum);
-  int again = threadIdx.x & 31;
-  asm volatile("" : "+v"(again));  // the row is found again here, not held in registers over the walk
-  const int x = w * 32 + again;
-  if (x < rows) {
-    if (part) {
-      float* to = part + (size_t)x * kHeadDim;
+
+    const Unit E = get(lds.unit[w][parity], P.T);
+    // Results go to memory in whole rows, through the part of the tile that this wave moves, in the buffer of the unit's last
+    // tile: its K when side 0 is done (side 1 has had it), its V when side 1 is. A row's 16-byte slot s lies at s ^ row % 16.
+    lsum = half_sum(lsum);
+    const bool whole = E.t0 == 0 && E.t1 == E.tiles;
+    const int ln = again(lane), hf = ln >> 5, r32 = ln & 31, x = w * 32 + r32;
+    int tok, head;
+    const int real = row_of(E, x, tok, head);
+    char* stage = (side ? lds.v[0] : lds.k[0]) + (buf ^ 1) * kTileBytes + wl * 32 * 256;
+    char* mine_row = stage + r32 * 256;
+    const int n_real = __builtin_popcountll(__ballot(real)) / 2;  // rows of the wave, the first ones
+    const int r4 = ln >> 4, slot = ln & 15;  // of rows 4 i + r4
+    // The values that were taken as 0, to the staged rows that see them: elements d0 .. d0 + n - 1, T each.
+    const auto add_odd = [&](auto type, int d0, int n, bool none) __attribute__((always_inline)) {
+      using V = decltype(type);
+      const int32_t* trow = P.table + (size_t)E.n * P.max_pages;
+      const int to = (int)min((int64_t)E.t1 * kTile, (int64_t)E.S.len) - 1;
+#pragma unroll 1
+      for (int t = odd_from; t <= to; ++t) {
+        const int32_t e = ld_uniform(trow + (t >> P.log2_page));
+        const uint64_t p = (uint32_t)e < (uint64_t)P.n_pages ? (uint32_t)e : 0u;
+        const uint16_t* v = P.vc + (p * page_bytes + (uint64_t)uniform(E.hh / P.parts) * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim;
+#pragma unroll 1
+        for (int i = hf * (n / 2); i < (hf + 1) * (n / 2); ++i) {
+          const uint32_t bits = (uint32_t)v[d0 + i] << 16;
+          if ((bits & 0x7f800000u) != 0x7f800000u || t > E.S.len - E.S.w + tok || none) continue;
+          const int byte = i * (int)sizeof(V);
+          V* x = reinterpret_cast<V*>(mine_row + (((byte >> 4) ^ (r32 & 15)) << 4) + (byte & 15));
+          *x = (V)((float)*x + __uint_as_float(bits));
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    if (!whole) {
+      float* part = P.part + ((size_t)b * 2 + (E.t0 == 0)) * P.part_rows * kRowFloats;
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
+      for (int hd = 0; hd < 2; ++hd) {
 #pragma unroll
-        for (int rg = 0; rg < 4; ++rg)
-          *reinterpret_cast<f32x4_t*>(to + 32 * dt + 8 * rg + 4 * half) =
+        for (int z = 0; z < 8; ++z) {
+          const int dt = 2 * hd + (z >> 2), rg = z & 3;
+          *reinterpret_cast<f32x4_t*>(mine_row + (((2 * z + hf) ^ (r32 & 15)) << 4)) =
               f32x4_t{o[dt][4 * rg], o[dt][4 * rg + 1], o[dt][4 * rg + 2], o[dt][4 * rg + 3]};
-      if (half == 0) {
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (odd_from != INT_MAX) add_odd(0.f, 64 * hd, 64, false);
+        f32x4_t v[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z)
+          v[z] = *reinterpret_cast<const f32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
+#pragma unroll
+        for (int z = 0; z < 8; ++z)
+          if (4 * z + r4 < n_real)
+            *reinterpret_cast<f32x4_t*>(part + (size_t)(w * 32 + 4 * z + r4) * kHeadDim + 64 * hd + 4 * slot) = v[z];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+      if (hf == 0 && real) {
         part[(size_t)P.part_rows * kHeadDim + x] = m;
         part[(size_t)P.part_rows * (kHeadDim + 1) + x] = lsum;
       }
     } else {
       // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
-      const int tok = x / heads;
-      const size_t out = (size_t)(row0 + first + tok) * P.Hq + g * P.G + hp * P.GP + (x - tok * heads);
       const bool none = lsum == 0.f;
-      uint16_t* to = P.o + out * kHeadDim;
+      const float inv = 1.f / lsum;
+      const int out = (E.row0 + tok) * P.Hq + head;
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
+      for (int z = 0; z < 16; ++z) {
+        const int dt = z >> 2, rg = z & 3;
+        uint32_t two[2];
 #pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : o[dt][4 * rg + e] / lsum;
-          store8(to + 32 * dt + 8 * rg + 4 * half, v, 1.f);
+        for (int e = 0; e < 2; ++e) {
+          const __bf16 lo = (__bf16)(none ? 0.f : o[dt][4 * rg + 2 * e] * inv), hi = (__bf16)(none ? 0.f : o[dt][4 * rg + 2 * e + 1] * inv);
+          two[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
         }
-      if (P.lse && half == 0) P.lse[out] = none ? -INFINITY : m * P.scale + logf(lsum);
-    }
-  }
-}
-
-__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads))) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_kernel(const ChunkParams P) {
-  __shared__ __attribute__((aligned(1024))) Lds lds;
-  __shared__ int64_t sums[kWaves];
-  __shared__ int64_t found_at;
-  __shared__ int found;
-  // Slots of the sequences: every thread a stretch of them.
-  const int heads = P.Hkv * P.parts;
-  const int per = (P.B + kThreads - 1) / kThreads;
-  const int n0 = min((int)threadIdx.x * per, P.B), n1 = min(n0 + per, P.B);
-  int64_t mine = 0, total = 0;
-  for (int n = n0; n < n1; ++n) mine += seq_of(P, n).slots() * heads;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t at = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up((long long)at, d, 64);
-    if (lane >= d) at += y;
-  }
-  if (lane == 63) sums[w] = at;
-  __syncthreads();
-  at -= mine;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < w) at += sums[i];
-    total += sums[i];
-  }
-  total = uniform(total);
-  const ChunkRanges R = chunk_ranges(total, P.grid, kShortest);
-  // Neighbouring ranges, which mostly share a KV head, go to one XCD.
-  if ((int)blockIdx.x >= R.n && threadIdx.x == 0) P.rec[blockIdx.x] = int4{-1, 0, 0, 0};  // no range has this number
-  const int per_xcd = (R.n + kNumXcd - 1) / kNumXcd, k = blockIdx.x / kNumXcd;
-  const int b = (blockIdx.x % kNumXcd) * per_xcd + k;
-  if (k >= per_xcd || b >= R.n) return;
-  const int64_t A = b * R.length, end = min(A + R.length, total);
-  if (A >= at && A < at + mine) {
-    int n = n0;
-    for (;; ++n) {
-      const int64_t t = seq_of(P, n).slots() * heads;
-      if (A < at + t) break;
-      at += t;
-    }
-    found = n;
-    found_at = at;
-  }
-  __syncthreads();
-  int n = uniform(found);
-  int64_t U = uniform(found_at);
-  int row0;
-  ChunkSeq S = seq_of_uniform(P, n, row0);
-  int64_t one = S.slots();
-  int hh = uniform((int)((A - U) / one));
-  U += hh * one;
-  int j = uniform(S.find(A - U));
-  U = uniform(U + S.start(j));
-  int4 rec = {-1, 0, 0, 0};
-  while (U < end) {
-    const int tiles = uniform(S.tiles(j)), t0 = uniform(chunk_tile0(A, U)), t1 = uniform(chunk_tile1(end, U, tiles));
-    if (t0 < t1) {
-      float* part = nullptr;
-      if (t0 > 0 || t1 < tiles) part = P.part + ((size_t)b * 2 + (t0 == 0)) * P.part_rows * kRowFloats;
-      if (t0 == 0 && t1 < tiles) rec = {n, hh, j, (int)((U + (int64_t)(tiles - 1) * kChunkTile) / R.length)};
-      walk(P, lds, S, n, row0, uniform(hh / P.parts), uniform(hh % P.parts), j, t0, t1, part);
-    }
-    U = uniform(U + S.keys(j) + kUnitSlots);
-    if (U >= end) break;
-    if (++j == S.units()) {
-      j = 0;
-      if (++hh == heads) {
-        hh = 0;
-        do S = seq_of_uniform(P, ++n, row0); while (S.w == 0);  // there are slots left, so there is one
+        *reinterpret_cast<u32x2_t*>(mine_row + ((z ^ (r32 & 15)) << 4) + 8 * hf) = u32x2_t{two[0], two[1]};
       }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (odd_from != INT_MAX) add_odd((__bf16)0.f, 0, kHeadDim, none);
+      u32x4_t v[8];
+      int to[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        v[z] = *reinterpret_cast<const u32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
+        to[z] = __shfl(out, 4 * z + r4, 64);
+      }
+#pragma unroll
+      for (int z = 0; z < 8; ++z)
+        if (4 * z + r4 < n_real) *reinterpret_cast<u32x4_t*>(P.o + (size_t)to[z] * kHeadDim + slot * 8) = v[z];
+      if (P.lse && hf == 0 && real) P.lse[out] = none ? -INFINITY : m * P.scale + logf(lsum);
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
+    if (threadIdx.x == 0 && E.t0 == 0 && !whole)
+      P.rec[b] = int4{E.n, E.hh, E.j, (int)((E.at + (int64_t)(E.tiles - 1) * kChunkTile) / lds.range[2])};
+    if (!more) break;
+    parity ^= 1;
   }
-  if (threadIdx.x == 0) P.rec[b] = rec;
+  if (side == 0) end_phase(false);  // as many barriers on both sides
 }
 
 constexpr int kJoinRows = 16;  // rows of a workgroup of the join, 32 lanes each
@@ -557,7 +710,7 @@ __global__ __launch_bounds__(kJoinRows * 32) void chunk_join_kernel(const ChunkP
   float v[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : O[e] / L;
-  store8(P.o + out * kHeadDim + t * 4, v, 1.f);
+  store4(P.o + out * kHeadDim + t * 4, v);
   if (P.lse && t == 0) P.lse[out] = none ? -INFINITY : M * P.scale + logf(L);
 }
 
@@ -576,19 +729,19 @@ hipError_t launch_chunk_attention(const ChunkShape& sh, const ChunkArgs& a, hipS
   int4* rec = static_cast<int4*>(a.workspace);
   float* part = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + kGrid * sizeof(int4));
   const int rows = part_rows(sh), T = chunk_tokens(sh.G), parts = chunk_parts(sh.G);
-  // Ranges that the rows can make: units of at most the table's tokens, at least one row each.
+  // Ranges that the rows can make (a power of two of them): units of at most the table's tokens, at least one row each.
   const long long units = std::min<long long>(sh.n_rows, (long long)sh.n_rows / T + sh.B) * sh.Hkv * parts;
-  const double slots = (double)units * ((double)sh.cap() + kUnitSlots);
-  const int grid = slots / kShortest + 1 < kGrid ? (int)(slots / kShortest) + 1 : kGrid;
+  const double ranges = (double)units * ((double)sh.cap() + kUnitSlots) / kShortest;
+  int log2_grid = kLog2Grid;
+  while (log2_grid > 3 && ranges <= (double)(1 << (log2_grid - 1))) --log2_grid;
+  const int grid = 1 << log2_grid;  // whole rounds over the XCDs
   const ChunkParams P{a.q, a.k_cache, a.v_cache, a.table, a.seq_lens, a.cu_new, part, rec, a.o, a.lse,
                       sh.B, sh.Hq, sh.Hkv, sh.G, chunk_heads(sh.G), parts, T,
-                      sh.max_pages, sh.log2_page, sh.n_rows, rows, grid, sh.q_stride, sh.n_pages,
+                      sh.max_pages, sh.log2_page, sh.n_rows, rows, log2_grid, sh.q_stride, sh.n_pages,
                       sh.scale, std::min(sh.scale * 1.4426950408889634f, FLT_MAX)};  // 0 times infinity is no logit
-  // whole rounds over the XCDs, so that every range has its workgroup
-  const int wgs = (grid + kNumXcd - 1) / kNumXcd * kNumXcd;
-  hipLaunchKernelGGL(chunk_kernel, dim3(wgs), dim3(kThreads), 0, stream, P);
+  hipLaunchKernelGGL(chunk_kernel, dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || grid == 1) return e;
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(chunk_join_kernel, dim3(grid, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * 32), 0, stream, P);
   return hipGetLastError();
 }

@@ -15,7 +15,7 @@ namespace cosa {
 constexpr int kChunkRows = 256;  // rows of a unit
 constexpr int kChunkTile = 128;  // keys of a tile
 // What taking up a unit costs beside its keys. At least a tile, so that a unit's last tile starts inside its slots.
-constexpr int kUnitSlots = 192;
+constexpr int kUnitSlots = 448;
 
 // Heads of a unit, units that share a group, and tokens of a unit, for G query heads per KV head.
 constexpr int chunk_heads(int G) { return G < kChunkRows ? G : kChunkRows; }
@@ -27,7 +27,7 @@ constexpr int chunk_tokens(int G) { return kChunkRows / chunk_heads(G); }
 struct ChunkSeq {
   int len, w, T;
 
-  constexpr int units() const { return (int)(((int64_t)w + T - 1) / T); }
+  constexpr int units() const { return (int)(((uint32_t)w + (uint32_t)T - 1u) / (uint32_t)T); }
   // Keys up to the last token of unit j.
   constexpr int keys(int j) const {
     const int64_t end = ((int64_t)j + 1) * T, k = (int64_t)len - w + (end < w ? end : w);
@@ -39,7 +39,7 @@ struct ChunkSeq {
   }
   // Slots in front of unit j (all units in front of it have T tokens).
   constexpr int64_t start(int j) const {
-    const int64_t ahead = (int64_t)w - len, z = ahead > 0 ? ahead / T : 0;  // units that end in front of token 0
+    const int64_t ahead = (int64_t)w - len, z = ahead > 0 ? (uint32_t)ahead / (uint32_t)T : 0;  // units that end in front of token 0
     int64_t s = (int64_t)kUnitSlots * j;
     if (j > z) s += (j - z) * ((int64_t)len - w) + (int64_t)T * ((int64_t)j * (j + 1) - z * (z + 1)) / 2;
     return s;
@@ -48,27 +48,20 @@ struct ChunkSeq {
     const int n = units();
     return n == 0 ? 0 : start(n - 1) + keys(n - 1) + kUnitSlots;
   }
-  // The unit that holds slot x < slots().
-  constexpr int find(int64_t x) const {
-    int lo = 0, hi = units() - 1;
-    while (lo < hi) {
-      const int mid = lo + (hi - lo + 1) / 2;
-      if (start(mid) <= x) lo = mid;
-      else hi = mid - 1;
-    }
-    return lo;
-  }
 };
 
-// The ranges of a line of `total` slots: at most `most` of them, `length` slots each but for the last one.
-struct ChunkRanges {
-  int64_t length;
-  int n;
-};
-constexpr ChunkRanges chunk_ranges(int64_t total, int most, int shortest) {
-  int64_t length = (total + most - 1) / most;
-  if (length < shortest) length = shortest;
-  return {length, (int)((total + length - 1) / length)};
+// The ranges of a line of `total` slots: 2^log2_most of `length` slots each; the last ones may have fewer, or none.
+constexpr int64_t chunk_range(int64_t total, int log2_most, int shortest) {
+  const int64_t length = (total + (1ll << log2_most) - 1) >> log2_most;
+  return length < shortest ? shortest : length;
+}
+
+// The largest i in [0, n) with start(i) <= x, for start(0) <= x and a start that does not fall, is searched for in rounds
+// of 64 places, a lane each: the first round looks at every search_step(n)-th place, the next ones at a 64th of that.
+constexpr int search_step(int n) {
+  int step = 1;
+  while ((int64_t)step * 64 < n) step *= 64;
+  return step;
 }
 
 // Tiles [t0, t1) that the range [a, b) has of a unit of `tiles` tiles whose slots start at u.

@@ -21,9 +21,22 @@ int keys(int len, int w, int T, int j) { return ChunkSeq{len, w, T}.keys(j); }
 int tiles(int len, int w, int T, int j) { return ChunkSeq{len, w, T}.tiles(j); }
 int64_t start(int len, int w, int T, int j) { return ChunkSeq{len, w, T}.start(j); }
 int64_t slots(int len, int w, int T) { return ChunkSeq{len, w, T}.slots(); }
-int find(int len, int w, int T, int64_t x) { return ChunkSeq{len, w, T}.find(x); }
-int64_t range_length(int64_t total, int most, int shortest) { return cosa::chunk_ranges(total, most, shortest).length; }
-int range_count(int64_t total, int most, int shortest) { return cosa::chunk_ranges(total, most, shortest).n; }
+// the unit that holds slot x, in rounds as the kernel's lanes search for it
+int find(int len, int w, int T, int64_t x) {
+  const ChunkSeq s{len, w, T};
+  const int n = s.units();
+  int first = 0;
+  for (int step = cosa::search_step(n); step; step /= 64) {
+    int hits = 0;
+    for (int lane = 0; lane < 64; ++lane) {
+      const int64_t i = (int64_t)first + (int64_t)lane * step;
+      hits += i < n && s.start((int)i) <= x;
+    }
+    first += (hits - 1) * step;
+  }
+  return first;
+}
+int64_t range_length(int64_t total, int log2_most, int shortest) { return cosa::chunk_range(total, log2_most, shortest); }
 int tile0(int64_t a, int64_t u) { return cosa::chunk_tile0(a, u); }
 int tile1(int64_t b, int64_t u, int tiles) { return cosa::chunk_tile1(b, u, tiles); }
 int unit_slots() { return cosa::kUnitSlots; }
@@ -40,7 +53,7 @@ def split(tmp_path_factory):
     lib = ctypes.CDLL(str(d / "split.so"))
     i, q = ctypes.c_int, ctypes.c_int64
     for name, args, res in (("start", [i, i, i, i], q), ("slots", [i, i, i], q), ("find", [i, i, i, q], i),
-                            ("range_length", [q, i, i], q), ("range_count", [q, i, i], i), ("tile0", [q, q], i),
+                            ("range_length", [q, i, i], q), ("tile0", [q, q], i),
                             ("tile1", [q, q, i], i)):
         getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
     return lib
@@ -74,8 +87,8 @@ def test_units_of_a_sequence(split, G):
         assert split.slots(length, w, T) == at
 
 
-@pytest.mark.parametrize("most,shortest", [(1, 128), (256, 256), (256, 128), (24, 512)])
-def test_every_tile_has_one_range(split, most, shortest):
+@pytest.mark.parametrize("log2_most,shortest", [(0, 128), (8, 256), (8, 128), (4, 512)])
+def test_every_tile_has_one_range(split, log2_most, shortest):
     rng = random.Random(11)
     for _ in range(30):
         T = rng.choice([1, 12, 36, 64, 256])
@@ -85,8 +98,9 @@ def test_every_tile_has_one_range(split, most, shortest):
             for j in range(split.units(length, w, T)):
                 units.append((at, split.tiles(length, w, T, j)))
                 at += split.keys(length, w, T, j) + split.unit_slots()
-        n, length = split.range_count(at, most, shortest), split.range_length(at, most, shortest)
-        assert n <= most and length >= shortest >= 128 and n * length >= at > (n - 1) * length if at else n == 0
+        length = split.range_length(at, log2_most, shortest)
+        n = -(-at // length)
+        assert n <= 1 << log2_most and length >= shortest >= 128
         owner = {}
         for b in range(n):
             lo, hi = b * length, min((b + 1) * length, at)
