@@ -97,6 +97,15 @@ __device__ __forceinline__ void store4(uint16_t* to, const float (&x)[4]) {
   *reinterpret_cast<u32x2_t*>(to) = u32x2_t{w[0], w[1]};
 }
 
+// The rounded m c that weights refer to, and what takes sums of such weights to the exact one.
+__device__ __forceinline__ float rounded(float m, float c) {
+#pragma clang fp contract(off)
+  return m * c;
+}
+__device__ __forceinline__ float exact_by(float m, float c) { return __builtin_amdgcn_exp2f(-fmaf(m, c, -rounded(m, c))); }
+constexpr float kLn2 = 0.69314718f;
+constexpr float kFar = 65536.f;  // the factor is within 2^-8 of 1 below
+
 // End of a phase: LDS accesses done (and, with full, this wave's copies landed), then the workgroup barrier.
 __device__ __forceinline__ void end_phase(bool full) {
   if (full) __builtin_amdgcn_s_waitcnt(kVmcntLgkm0);
@@ -111,7 +120,8 @@ struct Lds {
   char k[2][kTileBytes];
   int32_t unit[kWaves][2][16];  // a wave's unit and its next one
   int64_t range[3];             // the range's first slot and its end, and the length of all ranges
-  int odd[2][4];  // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
+  int row[kChunkRows];  // token and head of a row, for units of GP heads: token << 16 | head
+  int odd[2][4];        // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
 };
 
 // A unit of the line and the range's tiles of it.
@@ -284,7 +294,7 @@ void chunk_kernel(const ChunkParams P) {
   const auto fetch_from = [&](const Unit& u) __attribute__((always_inline)) {
     f_keys = uniform(u.S.keys(u.j));
     f_first = u.S.len - u.S.w + u.j * P.T;
-    f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)(u.hh / P.parts) * head_bytes));
+    f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)(P.parts == 1 ? u.hh : u.hh / P.parts) * head_bytes));
     f_row = P.table + (size_t)u.n * P.max_pages;
   };
   // Physical pages of the runs of tiles t .. t + 63, one tile a lane (run r: rows 32 wl + 16 r).
@@ -357,13 +367,24 @@ void chunk_kernel(const ChunkParams P) {
 
   // This lane's row of unit u: token and head (behind the unit's last token: that one again, which is not stored).
   const auto row_of = [&](const Unit& u, int x, int& tok, int& head) __attribute__((always_inline)) -> int {
-    const int hp = uniform(u.hh % P.parts), heads = heads_of(P, hp), tokens = min(P.T, u.S.w - u.j * P.T);
-    tok = x / heads;
-    head = uniform(u.hh / P.parts) * P.G + hp * P.GP + (x - tok * heads);
+    const int hp = P.parts == 1 ? 0 : uniform(u.hh % P.parts), g = P.parts == 1 ? u.hh : uniform(u.hh / P.parts);
+    const int heads = heads_of(P, hp), tokens = min(P.T, u.S.w - u.j * P.T);
+    const int packed = lds.row[x];
+    tok = packed >> 16;
+    head = packed & 0xffff;
+    if (heads != P.GP) {  // the last part of a large group
+      tok = x / heads;
+      head = x - tok * heads;
+    }
+    head += g * P.G + hp * P.GP;
     const bool real = tok < tokens;
     tok = u.j * P.T + min(tok, tokens - 1);
     return real;
   };
+  {
+    const int x = w * 32 + l32, tok = x / P.GP;
+    lds.row[x] = tok << 16 | (x - tok * P.GP);
+  }
   bf16x8_t qf[8];
   int pos;  // of the lane's row
   const auto load_q = [&](const Unit& u) __attribute__((always_inline)) {
@@ -397,8 +418,11 @@ void chunk_kernel(const ChunkParams P) {
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-    float m = -INFINITY;  // running maximum of the raw logits, the same in both halves
-    float lsum = 0.f;     // this half's share of the sum
+    // Running maximum of the raw logits, the same in both halves, and this half's share of the sum. A weight is exp2(s c -
+    // ref) with ref the rounded m c: one fma, and the rounding is the same factor for all of a row's weights. Where |ref|
+    // is large, that factor would be far from 1 (above 2^31, infinity or 0): from then on the wave takes exp2((s - m) c).
+    float m = -INFINITY, lsum = 0.f;
+    bool far = false;
     int odd_from = INT_MAX;  // first key of the first tile that was cleaned
     const int first_pos = D.S.len - D.S.w + D.j * P.T;
 
@@ -467,14 +491,24 @@ void chunk_kernel(const ChunkParams P) {
       X.mnew = fmaxf(m, half_max(mloc));
     };
 
-    const auto pv_half = [&](const Logits& X) __attribute__((always_inline)) {
+    const auto pv_half = [&](Logits& X) __attribute__((always_inline)) {
       if (!X.on) return;
-      const auto& s = X.s;
+      auto& s = X.s;
       const float mnew = X.mnew;
       __builtin_amdgcn_s_setprio(1);
-      // Differences are taken before the scale: a scaled maximum's rounding would be a factor of every weight.
       const float base = mnew == -INFINITY ? 0.f : mnew;
-      const float alpha = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
+      float ref = rounded(base, P.scale_log2);
+      float alpha = __builtin_amdgcn_exp2f(rounded(m, P.scale_log2) - ref);
+      if (far || __any(fabsf(ref) > kFar)) {
+        alpha = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
+        if (!far && m != -INFINITY) alpha *= exact_by(m, P.scale_log2);
+        far = true;
+#pragma unroll
+        for (int tt = 0; tt < kKeyTiles; ++tt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[tt][r] -= base;
+        ref = 0.f;
+      }
       m = mnew;
       if (__any(alpha != 1.f)) {
 #pragma unroll
@@ -489,7 +523,7 @@ void chunk_kernel(const ChunkParams P) {
       for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float pv = __builtin_amdgcn_exp2f((s[kc >> 1][8 * (kc & 1) + e] - base) * P.scale_log2);
+          const float pv = __builtin_amdgcn_exp2f(fmaf(s[kc >> 1][8 * (kc & 1) + e], P.scale_log2, -ref));
           rs += pv;
           pf[kc][e] = (__bf16)pv;
         }
@@ -605,13 +639,14 @@ void chunk_kernel(const ChunkParams P) {
     };
     if (!whole) {
       float* part = P.part + ((size_t)b * 2 + (E.t0 == 0)) * P.part_rows * kRowFloats;
+      const float by = far || m == -INFINITY ? 1.f : exact_by(m, P.scale_log2);
 #pragma unroll
       for (int hd = 0; hd < 2; ++hd) {
 #pragma unroll
         for (int z = 0; z < 8; ++z) {
           const int dt = 2 * hd + (z >> 2), rg = z & 3;
           *reinterpret_cast<f32x4_t*>(mine_row + (((2 * z + hf) ^ (r32 & 15)) << 4)) =
-              f32x4_t{o[dt][4 * rg], o[dt][4 * rg + 1], o[dt][4 * rg + 2], o[dt][4 * rg + 3]};
+              by * f32x4_t{o[dt][4 * rg], o[dt][4 * rg + 1], o[dt][4 * rg + 2], o[dt][4 * rg + 3]};
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (odd_from != INT_MAX) add_odd(0.f, 64 * hd, 64, false);
@@ -627,12 +662,18 @@ void chunk_kernel(const ChunkParams P) {
       }
       if (hf == 0 && real) {
         part[(size_t)P.part_rows * kHeadDim + x] = m;
-        part[(size_t)P.part_rows * (kHeadDim + 1) + x] = lsum;
+        part[(size_t)P.part_rows * (kHeadDim + 1) + x] = by * lsum;
       }
     } else {
       // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
       const bool none = lsum == 0.f;
-      const float inv = 1.f / lsum;
+      const float inv = none ? 0.f : 1.f / lsum;
+      if (__any(none)) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] = none ? 0.f : o[dt][r];
+      }
       const int out = (E.row0 + tok) * P.Hq + head;
 #pragma unroll
       for (int z = 0; z < 16; ++z) {
@@ -640,7 +681,7 @@ void chunk_kernel(const ChunkParams P) {
         uint32_t two[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const __bf16 lo = (__bf16)(none ? 0.f : o[dt][4 * rg + 2 * e] * inv), hi = (__bf16)(none ? 0.f : o[dt][4 * rg + 2 * e + 1] * inv);
+          const __bf16 lo = (__bf16)(o[dt][4 * rg + 2 * e] * inv), hi = (__bf16)(o[dt][4 * rg + 2 * e + 1] * inv);
           two[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
         }
         *reinterpret_cast<u32x2_t*>(mine_row + ((z ^ (r32 & 15)) << 4) + 8 * hf) = u32x2_t{two[0], two[1]};
@@ -657,7 +698,7 @@ void chunk_kernel(const ChunkParams P) {
 #pragma unroll
       for (int z = 0; z < 8; ++z)
         if (4 * z + r4 < n_real) *reinterpret_cast<u32x4_t*>(P.o + (size_t)to[z] * kHeadDim + slot * 8) = v[z];
-      if (P.lse && hf == 0 && real) P.lse[out] = none ? -INFINITY : m * P.scale + logf(lsum);
+      if (P.lse && hf == 0 && real) P.lse[out] = none ? -INFINITY : (far ? m * P.scale : rounded(m, P.scale_log2) * kLn2) + logf(lsum);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     if (threadIdx.x == 0 && E.t0 == 0 && !whole)
