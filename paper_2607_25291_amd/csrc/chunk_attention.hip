@@ -218,7 +218,7 @@ void chunk_kernel(const ChunkParams P) {
     if (begin < total) {
       if (begin >= at && begin < at + mine) {
         int n = n0;
-        for (;; ++n) {
+        for (; n < n1 - 1; ++n) {
           const int64_t t = seq_of(P, n).slots() * all_heads;
           if (begin < at + t) break;
           at += t;
@@ -263,7 +263,10 @@ void chunk_kernel(const ChunkParams P) {
       u.j = 0;
       if (++u.hh == all_heads) {
         u.hh = 0;
-        do u.S = seq_of_uniform(P, ++u.n, u.row0); while (u.S.w == 0);  // there are slots left, so there is one
+        do {  // there are slots left, so there is another sequence with rows
+          if (++u.n >= P.B) return false;
+          u.S = seq_of_uniform(P, u.n, u.row0);
+        } while (u.S.w == 0);
       }
     }
     settle(u, begin, end);

@@ -72,16 +72,27 @@ __global__ __launch_bounds__(kThreads) void clear_kernel(u32x4_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (size_t)gridDim.x * kThreads) p[i] = u32x4_t{0, 0, 0, 0};
 }
 
-// f(page number) for the pages that workgroup turn x of a table holds: kEntries entries of one row.
+// f(entry, page) for entries from, from + step, ... of a row below `held`, with pages outside the cache left out. Four loads
+// are in flight before the first is used: a store of f might change the next one's entry, for all the compiler knows.
+template <class F>
+__device__ __forceinline__ void for_pages(const int32_t* row, int from, int step, int held, long long n_pages, F&& f) {
+  for (int j0 = from; j0 < held; j0 += 4 * step) {
+    int p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = j0 + i * step < held ? row[j0 + i * step] : -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p[i] >= 0 && p[i] < n_pages) f(j0 + i * step, p[i]);
+  }
+}
+
+// f(page) for the pages that workgroup turn x of a table holds: kEntries entries of one row.
 template <class F>
 __device__ __forceinline__ void for_held(const int32_t* table, const int32_t* lens, int max_pages, int log2_page,
                                          long long n_pages, int x, F&& f) {
   const int turns = (max_pages + kEntries - 1) / kEntries, row = x / turns, j0 = x % turns * kEntries;
   const int j1 = min(j0 + kEntries, held_pages(lens[row], max_pages, log2_page));
-  for (int j = j0 + threadIdx.x; j < j1; j += kThreads) {
-    const int p = table[(size_t)row * max_pages + j];
-    if (p >= 0 && p < n_pages) f(p);
-  }
+  for_pages(table + (size_t)row * max_pages, j0 + (int)threadIdx.x, kThreads, j1, n_pages, [&](int, int p) { f(p); });
 }
 
 // ---- release
@@ -202,16 +213,20 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(PageCompactArgs 
     low = all;
   }
   const Plan P{(int)all, (int)low, min((int)(all - low), A.max_moves)};
+  // A thread's marks and the used pages in front of them; then neighbouring threads take neighbouring pages.
+  __shared__ uint32_t marks[kThreads], start[kThreads];
   const uint32_t bits = marks16<false>(W, blockIdx.x);
-  int c = (int)(before + block_scan<kThreads>(__popc(bits), waves, x));
-  const int page0 = blockIdx.x * kBlockPages + threadIdx.x * 16;
+  marks[threadIdx.x] = bits;
+  start[threadIdx.x] = before + block_scan<kThreads>(__popc(bits), waves, x);
+  __syncthreads();
   for (int i = 0; i < 16; ++i) {
-    const bool used = bits >> i & 1;
-    if (page0 + i < A.n_pages) {
-      if (used && page0 + i >= P.used) W.ranks[page0 + i] = P.used - 1 - c;
-      plan_page(A, P, page0 + i, used, c);
-    }
-    c += used;
+    const int at = i * kThreads + threadIdx.x, page = blockIdx.x * kBlockPages + at;
+    if (page >= A.n_pages) break;
+    const uint32_t m = marks[at >> 4];
+    const bool used = m >> (at & 15) & 1;
+    const int c = (int)(start[at >> 4] + __popc(m & ((1u << (at & 15)) - 1u)));
+    if (used && page >= P.used) W.ranks[page] = P.used - 1 - c;
+    plan_page(A, P, page, used, c);
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     *A.n_moves = P.moves;
@@ -225,14 +240,27 @@ __global__ __launch_bounds__(kThreads) void compact_table_kernel(PageCompactArgs
   const int per_row = (A.max_pages + kEntries - 1) / kEntries;
   for (int x = blockIdx.x; x < turns; x += gridDim.x) {
     const int row = x / per_row, j0 = x % per_row * kEntries, held = held_pages(A.seq_lens[row], A.max_pages, A.log2_page);
-    for (int j = j0 + threadIdx.x; j < min(j0 + kEntries, A.max_pages); j += kThreads) {
-      const size_t at = (size_t)row * A.max_pages + j;
-      int p = A.table[at];
-      if (j < held && p >= H.a && p < A.n_pages) {
-        const int r = W.ranks[p];
-        if (r < H.b) p = A.dst[r];
-      }
-      A.new_table[at] = p;
+    const int32_t* from = A.table + (size_t)row * A.max_pages;
+    int32_t* to = A.new_table + (size_t)row * A.max_pages;
+    constexpr int kEach = kEntries / kThreads;
+    int p[kEach], r[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int j = j0 + i * kThreads + (int)threadIdx.x;
+      p[i] = j < A.max_pages ? from[j] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int j = j0 + i * kThreads + (int)threadIdx.x;
+      r[i] = j < held && p[i] >= H.a && p[i] < A.n_pages ? W.ranks[p[i]] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if ((unsigned)r[i] < (unsigned)H.b) p[i] = A.dst[r[i]];  // every held page was ranked, if the table is still the same
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int j = j0 + i * kThreads + (int)threadIdx.x;
+      if (j < A.max_pages) to[j] = p[i];
     }
   }
 }
@@ -249,10 +277,7 @@ __device__ __forceinline__ void one_for_held(const int32_t* table, const int32_t
   const int lane = threadIdx.x & 63;
   for (int row = threadIdx.x >> 6; row < batch; row += kOneThreads / 64) {
     const int held = held_pages(lens[row], max_pages, log2_page);
-    for (int j = lane; j < held; j += 64) {
-      const int p = table[(size_t)row * max_pages + j];
-      if (p >= 0 && p < n_pages) f(p);
-    }
+    for_pages(table + (size_t)row * max_pages, lane, 64, held, n_pages, [&](int, int p) { f(p); });
   }
 }
 
@@ -315,14 +340,21 @@ __global__ __launch_bounds__(kOneThreads) void compact_one_kernel(PageCompactArg
   const int lane = threadIdx.x & 63;
   for (int row = threadIdx.x >> 6; row < A.batch; row += kOneThreads / 64) {
     const int held = held_pages(A.seq_lens[row], A.max_pages, A.log2_page);
-    for (int j = lane; j < A.max_pages; j += 64) {
-      const size_t e = (size_t)row * A.max_pages + j;
-      int p = A.table[e];
-      if (j < held && p >= P.used && p < A.n_pages) {
-        const int r = P.used - 1 - used_before(p);
-        if (r < P.moves) p = A.dst[r];
-      }
-      A.new_table[e] = p;
+    const int32_t* from = A.table + (size_t)row * A.max_pages;
+    int32_t* to = A.new_table + (size_t)row * A.max_pages;
+    for (int j0 = lane; j0 < A.max_pages; j0 += 4 * 64) {
+      int p[4], r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = j0 + i * 64 < A.max_pages ? from[j0 + i * 64] : -1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        r[i] = j0 + i * 64 < held && p[i] >= P.used && p[i] < A.n_pages ? P.used - 1 - used_before(p[i]) : -1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((unsigned)r[i] < (unsigned)P.moves) p[i] = A.dst[r[i]];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j0 + i * 64 < A.max_pages) to[j0 + i * 64] = p[i];
     }
   }
 }
