@@ -23,13 +23,18 @@ struct Header {  // in the workspace, written by one kernel for the next ones
   int a, b;
 };
 
-// The workspace: header, counts of the blocks, marks (release: two arrays of them), ranks (compact). Marks end with a
-// whole block.
+// 32 pages: which of them are in use, and how many in front of them.
+struct Word {
+  uint32_t bits, start;
+};
+
+// The workspace: header, counts of the blocks, marks, and a second array of them (release) or words (compact). All end
+// with a whole block.
 struct Pool {
   Header* header;
   int32_t* counts;
   uint8_t *marks, *marks2;
-  int32_t* ranks;
+  Word* words;
   int blocks;
   size_t bytes;
   Pool(void* ws, long long n_pages) {
@@ -40,8 +45,8 @@ struct Pool {
     counts = reinterpret_cast<int32_t*>(p + counts_at);
     marks = reinterpret_cast<uint8_t*>(p + marks_at);
     marks2 = marks + all;                                   // release
-    ranks = reinterpret_cast<int32_t*>(p + marks_at + all);  // compact
-    bytes = marks_at + 5 * all;
+    words = reinterpret_cast<Word*>(p + marks_at + all);    // compact
+    bytes = marks_at + 2 * all;
   }
 };
 
@@ -217,16 +222,16 @@ __global__ __launch_bounds__(kThreads) void compact_plan_kernel(PageCompactArgs 
   __shared__ uint32_t marks[kThreads], start[kThreads];
   const uint32_t bits = marks16<false>(W, blockIdx.x);
   marks[threadIdx.x] = bits;
-  start[threadIdx.x] = before + block_scan<kThreads>(__popc(bits), waves, x);
+  const uint32_t mine = before + block_scan<kThreads>(__popc(bits), waves, x), next = (uint32_t)__shfl_xor((int)bits, 1, 64);
+  start[threadIdx.x] = mine;
+  if ((threadIdx.x & 1) == 0) W.words[(blockIdx.x * kThreads + threadIdx.x) / 2] = Word{bits | next << 16, mine};
   __syncthreads();
   for (int i = 0; i < 16; ++i) {
     const int at = i * kThreads + threadIdx.x, page = blockIdx.x * kBlockPages + at;
     if (page >= A.n_pages) break;
     const uint32_t m = marks[at >> 4];
     const bool used = m >> (at & 15) & 1;
-    const int c = (int)(start[at >> 4] + __popc(m & ((1u << (at & 15)) - 1u)));
-    if (used && page >= P.used) W.ranks[page] = P.used - 1 - c;
-    plan_page(A, P, page, used, c);
+    plan_page(A, P, page, used, (int)(start[at >> 4] + __popc(m & ((1u << (at & 15)) - 1u))));
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     *A.n_moves = P.moves;
@@ -252,7 +257,11 @@ __global__ __launch_bounds__(kThreads) void compact_table_kernel(PageCompactArgs
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int j = j0 + i * kThreads + (int)threadIdx.x;
-      r[i] = j < held && p[i] >= H.a && p[i] < A.n_pages ? W.ranks[p[i]] : -1;
+      r[i] = -1;
+      if (j < held && p[i] >= H.a && p[i] < A.n_pages) {
+        const Word x = W.words[p[i] >> 5];
+        r[i] = H.a - 1 - (int)(x.start + __popc(x.bits & ((1u << (p[i] & 31)) - 1u)));
+      }
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
