@@ -29,7 +29,7 @@ constexpr int kTile = kChunkTile;
 constexpr int kKeyTiles = kTile / 32;
 constexpr int kTileBytes = kTile * kHeadDim * 2;  // one tensor's
 constexpr int kLog2Grid = 8, kGrid = 1 << kLog2Grid;  // workgroups that share the line: one a CU
-constexpr int kShortest = 256;                    // slots of the shortest range
+constexpr int kShortest = 256 * kFullSlots;           // slots of the shortest range
 constexpr int kRowFloats = kHeadDim + 2;          // of a partial result: O, maximum, sum
 
 // Partial results of workgroup b: slot 2 b of its first unit, which began in a range before, 2 b + 1 of its last one.
@@ -54,7 +54,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ ChunkSeq seq_of(const ChunkParams& P, int cu0, int cu1, int len, int& row0) {
   row0 = min(max(cu0, 0), P.n_rows);
   const int end = min(max(cu1, row0), P.n_rows);
-  return {min(max(len, 0), P.max_pages << P.log2_page), end - row0, P.T};
+  return {min(max(len, 0), P.max_pages << P.log2_page), end - row0, P.T, P.GP};
 }
 __device__ __forceinline__ ChunkSeq seq_of(const ChunkParams& P, int n) {
   int row0;
@@ -74,7 +74,7 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 __device__ __forceinline__ ChunkSeq seq_of_uniform(const ChunkParams& P, int n, int& row0) {
   const ChunkSeq S = seq_of(P, ld_uniform(P.cu_new + n), ld_uniform(P.cu_new + n + 1), ld_uniform(P.seq_lens + n), row0);
   row0 = uniform(row0);
-  return {uniform(S.len), uniform(S.w), P.T};
+  return {uniform(S.len), uniform(S.w), P.T, P.GP};
 }
 
 // Heads of unit part hp of a group.
@@ -124,31 +124,36 @@ struct Lds {
   int odd[2][4];        // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
 };
 
-// A unit of the line and the range's tiles of it.
+// A unit of the line and the range's tiles of it. I: the type of slots, 32 bits where they hold all of them (a small call
+// 20.7 us with 64 bits).
+template <class I>
 struct Unit {
   ChunkSeq S;
   int n, row0;  // sequence, its first row
   int hh, j;    // KV head and part, unit of these
-  int64_t at;   // its first slot
+  I at;         // its first slot
   int tiles, t0, t1;
 };
 // Units wait in LDS, one copy a wave: in scalar registers, two of them would push other values out.
-__device__ __forceinline__ void put(int32_t* to, const Unit& u) {
+template <class I>
+__device__ __forceinline__ void put(int32_t* to, const Unit<I>& u) {
   if ((threadIdx.x & 63) == 0) {
     int4* p = reinterpret_cast<int4*>(to);
     p[0] = int4{u.S.len, u.S.w, u.n, u.row0};
-    p[1] = int4{u.hh, u.j, (int)u.at, (int)(u.at >> 32)};
+    p[1] = int4{u.hh, u.j, (int)u.at, (int)((int64_t)u.at >> 32)};
     p[2] = int4{u.tiles, u.t0, u.t1, 0};
   }
 }
-__device__ __forceinline__ Unit get(const int32_t* from, int T) {
+template <class I>
+__device__ __forceinline__ Unit<I> get(const int32_t* from, const ChunkParams& P) {
   asm volatile("" ::: "memory");
   const int4* p = reinterpret_cast<const int4*>(from);
   const int4 a = p[0], b = p[1], c = p[2];
-  return {{uniform(a.x), uniform(a.y), T}, uniform(a.z), uniform(a.w), uniform(b.x), uniform(b.y),
-          (int64_t)(uint32_t)uniform(b.z) | (int64_t)uniform(b.w) << 32, uniform(c.x), uniform(c.y), uniform(c.z)};
+  return {{uniform(a.x), uniform(a.y), P.T, P.GP}, uniform(a.z), uniform(a.w), uniform(b.x), uniform(b.y),
+          uniform((I)((int64_t)(uint32_t)b.z | (int64_t)b.w << 32)), uniform(c.x), uniform(c.y), uniform(c.z)};
 }
 
+template <class I>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads))) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void chunk_kernel(const ChunkParams P) {
   __shared__ __attribute__((aligned(1024))) Lds lds;
@@ -158,53 +163,69 @@ void chunk_kernel(const ChunkParams P) {
   // The range of this workgroup, and its first unit. Slots of the sequences: one a lane, every wave for itself, or a
   // stretch of them a thread.
   const int all_heads = P.Hkv * P.parts;
-  Unit D;
-  int64_t begin, end, total = 0;
+  int cu0 = 0, cu1 = 0, tokens = 0;
+  if (P.B <= 64 && lane < P.B) {
+    cu0 = P.cu_new[lane];
+    cu1 = P.cu_new[lane + 1];
+    tokens = P.seq_lens[lane];
+  }
+  {  // while these load
+    const int x = w * 32 + l32, tok = x / P.GP;
+    lds.row[x] = tok << 16 | (x - tok * P.GP);
+  }
+  Unit<I> D;
+  I begin, end, total = 0;
   int b;
   const auto place = [&]() __attribute__((always_inline)) {
-    const int64_t length = chunk_range(total, P.log2_grid, kShortest);
+    const I length = chunk_range<I>(total, P.log2_grid, kShortest);
     // Neighbouring ranges, which mostly share a KV head, go to one XCD: of all ranges, or of those with slots.
     const int per_xcd = length > kShortest ? gridDim.x / kNumXcd : (int)((total + kShortest * kNumXcd - 1) / (kShortest * kNumXcd));
     const int k = blockIdx.x / kNumXcd;
     b = k < per_xcd ? (blockIdx.x % kNumXcd) * per_xcd + k : (int)blockIdx.x;
-    begin = k < per_xcd ? b * length : total;
+    begin = k < per_xcd ? min((I)b * length, total) : total;
     end = min(begin + length, total);
-    if (threadIdx.x == 0) lds.range[2] = length;
+    if (threadIdx.x == 0) {
+      P.rec[b] = int4{-1, 0, 0, 0};
+      lds.range[0] = begin;
+      lds.range[1] = end;
+      lds.range[2] = length;
+    }
   };
-  const auto of = [&](int64_t x, int l) __attribute__((always_inline)) -> int64_t {
-    return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, l) | (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32;
+  const auto of = [&](I x, int l) __attribute__((always_inline)) -> I {
+    if (sizeof(I) == 4) return __builtin_amdgcn_readlane((int)x, l);
+    return (I)((int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, l) |
+               (int64_t)__builtin_amdgcn_readlane((int)((int64_t)x >> 32), l) << 32);
   };
-  const auto scan = [&](int64_t x) __attribute__((always_inline)) {
+  const auto scan = [&](I x) __attribute__((always_inline)) -> I {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up((long long)x, d, 64);
+      const I y = (I)__shfl_up(x, d, 64);
       if (lane >= d) x += y;
     }
     return x;
   };
   if (P.B <= 64) {
-    int row0 = 0;
-    ChunkSeq S{0, 0, P.T};
-    if (lane < P.B) S = seq_of(P, P.cu_new[lane], P.cu_new[lane + 1], P.seq_lens[lane], row0);
-    const int64_t mine = S.slots() * all_heads;
-    const int64_t at = P.B == 1 ? mine : scan(mine);
+    int row0;
+    ChunkSeq S = seq_of(P, cu0, cu1, tokens, row0);
+    if (lane >= P.B) S.w = 0;
+    const I mine = S.template slots<I>() * all_heads;
+    const I at = P.B == 1 ? mine : scan(mine);
     total = of(at, P.B - 1);
     place();
-    if (begin < total) {
-      D.n = __builtin_popcountll(__ballot(lane < P.B && at <= begin));  // the sequences that end in front of it
-      D.at = of(at - mine, D.n);
-      D.S = ChunkSeq{__builtin_amdgcn_readlane(S.len, D.n), __builtin_amdgcn_readlane(S.w, D.n), P.T};
-      D.row0 = __builtin_amdgcn_readlane(row0, D.n);
-    }
+    if (begin >= total) return;
+    D.n = __builtin_popcountll(__ballot(lane < P.B && at <= begin));  // the sequences that end in front of it
+    D.at = of(at - mine, D.n);
+    D.S = ChunkSeq{__builtin_amdgcn_readlane(S.len, D.n), __builtin_amdgcn_readlane(S.w, D.n), P.T, P.GP};
+    D.row0 = __builtin_amdgcn_readlane(row0, D.n);
   } else {
-    __shared__ int64_t sums[kWaves];
-    __shared__ int64_t found_at;
+    __shared__ I sums[kWaves];
+    __shared__ I found_at;
     __shared__ int found;
     const int per = (P.B + kThreads - 1) / kThreads;
     const int n0 = min((int)threadIdx.x * per, P.B), n1 = min(n0 + per, P.B);
-    int64_t mine = 0;
-    for (int n = n0; n < n1; ++n) mine += seq_of(P, n).slots() * all_heads;
-    int64_t at = scan(mine);
+    I mine = 0;
+    for (int n = n0; n < n1; ++n) mine += seq_of(P, n).template slots<I>() * all_heads;
+    I at = scan(mine);
     if (lane == 63) sums[w] = at;
     __syncthreads();
     at -= mine;
@@ -215,28 +236,25 @@ void chunk_kernel(const ChunkParams P) {
     }
     total = uniform(total);
     place();
-    if (begin < total) {
-      if (begin >= at && begin < at + mine) {
-        int n = n0;
-        for (; n < n1 - 1; ++n) {
-          const int64_t t = seq_of(P, n).slots() * all_heads;
-          if (begin < at + t) break;
-          at += t;
-        }
-        found = n;
-        found_at = at;
+    if (begin >= total) return;
+    if (begin >= at && begin < at + mine) {
+      int n = n0;
+      for (; n < n1 - 1; ++n) {
+        const I t = seq_of(P, n).template slots<I>() * all_heads;
+        if (begin < at + t) break;
+        at += t;
       }
-      __syncthreads();
-      D.n = uniform(found);
-      D.at = uniform(found_at);
-      D.S = seq_of_uniform(P, D.n, D.row0);
+      found = n;
+      found_at = at;
     }
+    __syncthreads();
+    D.n = uniform(found);
+    D.at = uniform(found_at);
+    D.S = seq_of_uniform(P, D.n, D.row0);
   }
-  if (threadIdx.x == 0) P.rec[b] = int4{-1, 0, 0, 0};
-  if (begin >= total) return;
   {
     // largest i in [0, n) with start(i) <= x
-    const auto search = [&](int n, int64_t x, auto&& start) __attribute__((always_inline)) -> int {
+    const auto search = [&](int n, I x, auto&& start) __attribute__((always_inline)) -> int {
       int first = 0;
       for (int step = search_step(n); step; step /= 64) {
         const int64_t i = (int64_t)first + (int64_t)lane * step;
@@ -244,20 +262,22 @@ void chunk_kernel(const ChunkParams P) {
       }
       return first;
     };
-    const int64_t one = uniform(D.S.slots());
-    D.hh = search(all_heads, begin - D.at, [&](int i) { return one * i; });
+    const I one = uniform(D.S.template slots<I>());
+    D.hh = all_heads == 1 ? 0 : search(all_heads, begin - D.at, [&](int i) { return one * i; });
     D.at += D.hh * one;
-    D.j = search(D.S.units(), begin - D.at, [&](int i) { return D.S.start(i); });
-    D.at = uniform(D.at + D.S.start(D.j));
+    const int units = uniform(D.S.units());
+    D.j = units == 1 ? 0 : search(units, begin - D.at, [&](int i) { return D.S.template start<I>(i); });
+    D.at = uniform(D.at + D.S.template start<I>(D.j));
   }
-  const auto settle = [&](Unit& u, int64_t begin, int64_t end) __attribute__((always_inline)) {
+  const auto settle = [&](Unit<I>& u, I begin, I end) __attribute__((always_inline)) {
     u.tiles = uniform(u.S.tiles(u.j));
-    u.t0 = uniform(chunk_tile0(begin, u.at));
-    u.t1 = uniform(chunk_tile1(end, u.at, u.tiles));
+    const int key_slots = u.S.key_slots(u.j);
+    u.t0 = uniform(chunk_tile0<I>(begin, u.at, key_slots));
+    u.t1 = uniform(chunk_tile1<I>(end, u.at, key_slots, u.tiles));
   };
   // The next unit of the range (its first one may have no tile here).
-  const auto advance = [&](Unit& u, int64_t begin, int64_t end) __attribute__((always_inline)) -> bool {
-    u.at = uniform(u.at + u.S.keys(u.j) + kUnitSlots);
+  const auto advance = [&](Unit<I>& u, I begin, I end) __attribute__((always_inline)) -> bool {
+    u.at = uniform(u.at + u.S.template cost<I>(u.j));
     if (u.at >= end) return false;
     if (++u.j == u.S.units()) {
       u.j = 0;
@@ -273,10 +293,6 @@ void chunk_kernel(const ChunkParams P) {
     return true;
   };
   settle(D, begin, end);
-  if (threadIdx.x == 0) {
-    lds.range[0] = begin;
-    lds.range[1] = end;
-  }
   if (D.t0 >= D.t1 && !advance(D, begin, end)) return;
 
   // Copies. Waves w and w + 4 share a SIMD; side 1 (w >= 4) runs one phase behind. Side 0 moves K, side 1 V: wave wl rows 32
@@ -294,7 +310,7 @@ void chunk_kernel(const ChunkParams P) {
   uint64_t f_cache;
   const int32_t* f_row;
   int pg[2];
-  const auto fetch_from = [&](const Unit& u) __attribute__((always_inline)) {
+  const auto fetch_from = [&](const Unit<I>& u) __attribute__((always_inline)) {
     f_keys = uniform(u.S.keys(u.j));
     f_first = u.S.len - u.S.w + u.j * P.T;
     f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)(P.parts == 1 ? u.hh : u.hh / P.parts) * head_bytes));
@@ -369,7 +385,7 @@ void chunk_kernel(const ChunkParams P) {
                    8 * (li & 1);
 
   // This lane's row of unit u: token and head (behind the unit's last token: that one again, which is not stored).
-  const auto row_of = [&](const Unit& u, int x, int& tok, int& head) __attribute__((always_inline)) -> int {
+  const auto row_of = [&](const Unit<I>& u, int x, int& tok, int& head) __attribute__((always_inline)) -> int {
     const int hp = P.parts == 1 ? 0 : uniform(u.hh % P.parts), g = P.parts == 1 ? u.hh : uniform(u.hh / P.parts);
     const int heads = heads_of(P, hp), tokens = min(P.T, u.S.w - u.j * P.T);
     const int packed = lds.row[x];
@@ -384,13 +400,9 @@ void chunk_kernel(const ChunkParams P) {
     tok = u.j * P.T + min(tok, tokens - 1);
     return real;
   };
-  {
-    const int x = w * 32 + l32, tok = x / P.GP;
-    lds.row[x] = tok << 16 | (x - tok * P.GP);
-  }
   bf16x8_t qf[8];
   int pos;  // of the lane's row
-  const auto load_q = [&](const Unit& u) __attribute__((always_inline)) {
+  const auto load_q = [&](const Unit<I>& u) __attribute__((always_inline)) {
     int tok, head;
     const int ln = again(lane);
     row_of(u, w * 32 + (ln & 31), tok, head);
@@ -412,7 +424,7 @@ void chunk_kernel(const ChunkParams P) {
   int parity = 0;
   put(lds.unit[w][0], D);
   for (;;) {
-    const Unit D = get(lds.unit[w][parity], P.T);
+    const Unit<I> D = get<I>(lds.unit[w][parity], P);
     const bool live = w * 32 < min(P.T, D.S.w - D.j * P.T) * heads_of(P, uniform(D.hh % P.parts));
     const int pos_low = uniform(pos);  // of the wave's rows
     const int pos_top = __builtin_amdgcn_readlane(pos, 31);
@@ -578,8 +590,8 @@ void chunk_kernel(const ChunkParams P) {
       const bool last = t + 1 == t1;
       int to = t + 1;
       if (last) {
-        Unit N = get(lds.unit[w][parity], P.T);
-        more = advance(N, uniform(lds.range[0]), uniform(lds.range[1]));
+        Unit<I> N = get<I>(lds.unit[w][parity], P);
+        more = advance(N, uniform((I)lds.range[0]), uniform((I)lds.range[1]));
         i = 0;
         to = 0;
         if (more) {
@@ -594,7 +606,7 @@ void chunk_kernel(const ChunkParams P) {
       const bool fetch = !last || more;
       Logits X;
       qk_half(t, X);
-      if (last && more) load_q(get(lds.unit[w][parity ^ 1], P.T));  // its registers are free from here on
+      if (last && more) load_q(get<I>(lds.unit[w][parity ^ 1], P));  // its registers are free from here on
       if (fetch) copy(to, i, buf ^ 1);
       end_phase(false);
       if (first_pos - t * kTile < kTile - 1) {
@@ -607,7 +619,7 @@ void chunk_kernel(const ChunkParams P) {
       buf ^= 1;
     }
 
-    const Unit E = get(lds.unit[w][parity], P.T);
+    const Unit<I> E = get<I>(lds.unit[w][parity], P);
     // Results go to memory in whole rows, through the part of the tile that this wave moves, in the buffer of the unit's last
     // tile: its K when side 0 is done (side 1 has had it), its V when side 1 is. A row's 16-byte slot s lies at s ^ row % 16.
     lsum = half_sum(lsum);
@@ -705,7 +717,7 @@ void chunk_kernel(const ChunkParams P) {
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     if (threadIdx.x == 0 && E.t0 == 0 && !whole)
-      P.rec[b] = int4{E.n, E.hh, E.j, (int)((E.at + (int64_t)(E.tiles - 1) * kChunkTile) / lds.range[2])};
+      P.rec[b] = int4{E.n, E.hh, E.j, (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
     if (!more) break;
     parity ^= 1;
   }
@@ -775,7 +787,7 @@ hipError_t launch_chunk_attention(const ChunkShape& sh, const ChunkArgs& a, hipS
   const int rows = part_rows(sh), T = chunk_tokens(sh.G), parts = chunk_parts(sh.G);
   // Ranges that the rows can make (a power of two of them): units of at most the table's tokens, at least one row each.
   const long long units = std::min<long long>(sh.n_rows, (long long)sh.n_rows / T + sh.B) * sh.Hkv * parts;
-  const double ranges = (double)units * ((double)sh.cap() + kUnitSlots) / kShortest;
+  const double ranges = (double)units * ((double)sh.cap() + kUnitKeys) * kFullSlots / kShortest;
   int log2_grid = kLog2Grid;
   while (log2_grid > 3 && ranges <= (double)(1 << (log2_grid - 1))) --log2_grid;
   const int grid = 1 << log2_grid;  // whole rounds over the XCDs
@@ -783,7 +795,10 @@ hipError_t launch_chunk_attention(const ChunkShape& sh, const ChunkArgs& a, hipS
                       sh.B, sh.Hq, sh.Hkv, sh.G, chunk_heads(sh.G), parts, T,
                       sh.max_pages, sh.log2_page, sh.n_rows, rows, log2_grid, sh.q_stride, sh.n_pages,
                       sh.scale, std::min(sh.scale * 1.4426950408889634f, FLT_MAX)};  // 0 times infinity is no logit
-  hipLaunchKernelGGL(chunk_kernel, dim3(grid), dim3(kThreads), 0, stream, P);
+  if (chunk_narrow(sh.B, sh.n_rows, sh.cap(), (long long)sh.Hkv * parts, T))
+    hipLaunchKernelGGL(chunk_kernel<int32_t>, dim3(grid), dim3(kThreads), 0, stream, P);
+  else
+    hipLaunchKernelGGL(chunk_kernel<int64_t>, dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(chunk_join_kernel, dim3(grid, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * 32), 0, stream, P);

@@ -3,9 +3,9 @@
 //
 // A unit is (sequence, KV head, up to 256 query heads of its group, T tokens): its rows are the T tokens' heads, T as
 // many whole tokens as 256 rows hold. It walks the keys up to its last token in tiles of 128. Units lie one
-// behind the other on a line of slots, a slot a key and kUnitSlots more for a unit; the line is cut into equal
-// ranges, and a range has the tiles whose first slot it holds. So every tile has one owner whatever the lengths are, and
-// a unit's place on the line has a closed form.
+// behind the other on a line of slots, each as long as it takes in time; the line is cut into equal ranges, and a range has
+// the tiles whose first slot it holds. So every tile has one owner whatever the lengths are, and a unit's place on the
+// line has a closed form: only the last unit of a sequence has fewer than T tokens.
 #pragma once
 
 #include <stdint.h>
@@ -14,8 +14,13 @@ namespace cosa {
 
 constexpr int kChunkRows = 256;  // rows of a unit
 constexpr int kChunkTile = 128;  // keys of a tile
-// What taking up a unit costs beside its keys. At least a tile, so that a unit's last tile starts inside its slots.
-constexpr int kUnitSlots = 448;
+// Slots of a key in a unit, and in one whose rows leave half of the workgroup idle (its tiles take some 5,000 cycles, others
+// 7,000). Counted alike, the ranges of one-token units end early: 48 sequences of which 43 add one token 9 % longer.
+constexpr int kFullSlots = 3, kFewSlots = 2;
+// What taking up a unit costs beside its keys, in keys; at least a tile, so that a unit's last tile starts inside its
+// slots. 19 prompts of up to 4K tokens with 192 / 320 / 448 / 640 keys: 927 / 781 / 723 / 742 us (prefetches across units are
+// in these); with 448 the ranges end within 3 % of each other.
+constexpr int kUnitKeys = 448;
 
 // Heads of a unit, units that share a group, and tokens of a unit, for G query heads per KV head.
 constexpr int chunk_heads(int G) { return G < kChunkRows ? G : kChunkRows; }
@@ -23,9 +28,9 @@ constexpr int chunk_parts(int G) { return (G + kChunkRows - 1) / kChunkRows; }
 constexpr int chunk_tokens(int G) { return kChunkRows / chunk_heads(G); }
 
 // One sequence's units for one KV head and part: `len` tokens, the last `w` of them new (w > len: the first w - len
-// stand in front of token 0 and see nothing), T new tokens a unit.
+// stand in front of token 0 and see nothing), T new tokens of `heads` rows a unit. I: int64_t, or int32_t where chunk_narrow().
 struct ChunkSeq {
-  int len, w, T;
+  int len, w, T, heads;
 
   constexpr int units() const { return (int)(((uint32_t)w + (uint32_t)T - 1u) / (uint32_t)T); }
   // Keys up to the last token of unit j.
@@ -37,22 +42,42 @@ struct ChunkSeq {
     const int t = (int)(((int64_t)keys(j) + kChunkTile - 1) / kChunkTile);
     return t > 0 ? t : 1;
   }
-  // Slots in front of unit j (all units in front of it have T tokens).
-  constexpr int64_t start(int j) const {
-    const int64_t ahead = (int64_t)w - len, z = ahead > 0 ? (uint32_t)ahead / (uint32_t)T : 0;  // units that end in front of token 0
-    int64_t s = (int64_t)kUnitSlots * j;
-    if (j > z) s += (j - z) * ((int64_t)len - w) + (int64_t)T * ((int64_t)j * (j + 1) - z * (z + 1)) / 2;
-    return s;
+  constexpr int key_slots(int j) const {
+    const int64_t left = (int64_t)w - (int64_t)j * T;
+    return (left < T ? left : T) * heads <= kChunkRows / 2 ? kFewSlots : kFullSlots;
   }
-  constexpr int64_t slots() const {  // of all units
+  template <class I>
+  constexpr I cost(int j) const {
+    return ((I)keys(j) + kUnitKeys) * key_slots(j);
+  }
+  // Slots in front of unit j (all units in front of it have T tokens, more than half of the rows).
+  template <class I>
+  constexpr I start(int j) const {
+    const int ahead = w - len, z = ahead > 0 ? (int)((uint32_t)ahead / (uint32_t)T) : 0;  // units that end in front of token 0
+    I s = (I)kUnitKeys * j;
+    if (j > z) s += (I)(j - z) * (len - w) + (I)T * ((I)j * (j + 1) - (I)z * (z + 1)) / 2;
+    return s * kFullSlots;
+  }
+  template <class I>
+  constexpr I slots() const {  // of all units
     const int n = units();
-    return n == 0 ? 0 : start(n - 1) + keys(n - 1) + kUnitSlots;
+    return n == 0 ? 0 : start<I>(n - 1) + cost<I>(n - 1);
   }
 };
 
+// Whether 31 bits hold every sum of slots of a call, and of their terms: `batch` sequences of up to n_rows rows (they may
+// overlap) and `cap` tokens, units for `heads` KV heads and parts.
+constexpr bool chunk_narrow(int64_t batch, int64_t n_rows, int64_t cap, int64_t heads, int T) {
+  const int64_t units = n_rows / T + 1, most = (cap > n_rows ? cap : n_rows) + kUnitKeys;  // of a sequence; keys of a unit
+  const double limit = 2147483648.0;
+  return (double)units * (double)(n_rows + 2 * T) < limit &&
+         (double)units * (double)most * kFullSlots * (double)heads * (double)batch < limit / 2;
+}
+
 // The ranges of a line of `total` slots: 2^log2_most of `length` slots each; the last ones may have fewer, or none.
-constexpr int64_t chunk_range(int64_t total, int log2_most, int shortest) {
-  const int64_t length = (total + (1ll << log2_most) - 1) >> log2_most;
+template <class I>
+constexpr I chunk_range(I total, int log2_most, int shortest) {
+  const I length = (total + ((I)1 << log2_most) - 1) >> log2_most;
   return length < shortest ? shortest : length;
 }
 
@@ -64,10 +89,19 @@ constexpr int search_step(int n) {
   return step;
 }
 
-// Tiles [t0, t1) that the range [a, b) has of a unit of `tiles` tiles whose slots start at u.
-constexpr int chunk_tile0(int64_t a, int64_t u) { return a > u ? (int)((a - u + kChunkTile - 1) / kChunkTile) : 0; }
-constexpr int chunk_tile1(int64_t b, int64_t u, int tiles) {
-  const int64_t t = (b - u + kChunkTile - 1) / kChunkTile;
+// Tiles [t0, t1) that the range [a, b) has of a unit of `tiles` tiles whose slots start at u, key_slots a key.
+template <class I>
+constexpr I chunk_tiles_ahead(I slots, int key_slots) {
+  return key_slots == kFewSlots ? (slots + kChunkTile * kFewSlots - 1) / (kChunkTile * kFewSlots)
+                                : (slots + kChunkTile * kFullSlots - 1) / (kChunkTile * kFullSlots);
+}
+template <class I>
+constexpr int chunk_tile0(I a, I u, int key_slots) {
+  return a > u ? (int)chunk_tiles_ahead<I>(a - u, key_slots) : 0;
+}
+template <class I>
+constexpr int chunk_tile1(I b, I u, int key_slots, int tiles) {
+  const I t = chunk_tiles_ahead<I>(b - u, key_slots);
   return t < tiles ? (int)t : tiles;
 }
 
