@@ -29,7 +29,8 @@ constexpr int kTile = kChunkTile;
 constexpr int kKeyTiles = kTile / 32;
 constexpr int kTileBytes = kTile * kHeadDim * 2;  // one tensor's
 constexpr int kLog2Grid = 8, kGrid = 1 << kLog2Grid;  // workgroups that share the line: one a CU
-constexpr int kShortest = 256 * kFullSlots;           // slots of the shortest range
+constexpr int kShortest = 512;                        // slots of the shortest range: at least a tile's
+static_assert(kShortest >= kTile * kFullSlots, "every range but the last holds the start of a tile");
 constexpr int kRowFloats = kHeadDim + 2;          // of a partial result: O, maximum, sum
 
 // Partial results of workgroup b: slot 2 b of its first unit, which began in a range before, 2 b + 1 of its last one.
@@ -742,18 +743,20 @@ __global__ __launch_bounds__(kJoinRows * 32) void chunk_join_kernel(const ChunkP
   const auto part = [&](int i) { return P.part + ((size_t)(blockIdx.x + i) * 2 + (i == 0)) * stride; };
   float M = -INFINITY, L = 0.f;
   f32x4_t O = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < n_parts; i0 += 4) {
-    float m[4], l[4];
-    f32x4_t o[4];
+  // N parts at a time, so that their loads wait side by side: two where there are no more, as in most long calls.
+  const auto add = [&](auto nc, int i0) __attribute__((always_inline)) {
+    constexpr int N = decltype(nc)::value;
+    float m[N], l[N];
+    f32x4_t o[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {  // behind the last part: that one again, without weight
+    for (int i = 0; i < N; ++i) {  // behind the last part: that one again, without weight
       const float* p = part(min(i0 + i, n_parts - 1));
       m[i] = p[(size_t)P.part_rows * kHeadDim + x];
       l[i] = p[(size_t)P.part_rows * (kHeadDim + 1) + x];
       o[i] = *reinterpret_cast<const f32x4_t*>(p + (size_t)x * kHeadDim + t * 4);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
       if (i0 + i >= n_parts) break;
       const float mx = fmaxf(M, m[i]), base = mx == -INFINITY ? 0.f : mx;
       const float a = __builtin_amdgcn_exp2f((M - base) * P.scale_log2), c = __builtin_amdgcn_exp2f((m[i] - base) * P.scale_log2);
@@ -761,7 +764,10 @@ __global__ __launch_bounds__(kJoinRows * 32) void chunk_join_kernel(const ChunkP
       O = a * O + c * o[i];
       M = mx;
     }
-  }
+  };
+  if (n_parts <= 2) add(std::integral_constant<int, 2>{}, 0);
+  else
+    for (int i0 = 0; i0 < n_parts; i0 += 8) add(std::integral_constant<int, 8>{}, i0);
   const bool none = L == 0.f;
   float v[4];
 #pragma unroll
