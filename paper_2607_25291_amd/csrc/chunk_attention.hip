@@ -38,7 +38,7 @@ struct ChunkParams {
   const uint16_t *q, *kc, *vc;
   const int32_t *table, *seq_lens, *cu_new;
   float* part;
-  int4* rec;  // [kGrid]: a unit that begins in range b and ends in another one: sequence, head and part, unit, last range
+  int4* rec;  // [kGrid]: a unit that begins in range b and ends in another one: first row, rows (0: none), head and part, last range
   uint16_t* o;
   float* lse;
   int B, Hq, Hkv, G, GP, parts, T;  // GP: heads of a unit
@@ -186,7 +186,7 @@ void chunk_kernel(const ChunkParams P) {
     begin = k < per_xcd ? min((I)b * length, total) : total;
     end = min(begin + length, total);
     if (threadIdx.x == 0) {
-      P.rec[b] = int4{-1, 0, 0, 0};
+      P.rec[b] = int4{0, 0, 0, 0};
       lds.range[0] = begin;
       lds.range[1] = end;
       lds.range[2] = length;
@@ -718,62 +718,85 @@ void chunk_kernel(const ChunkParams P) {
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     if (threadIdx.x == 0 && E.t0 == 0 && !whole)
-      P.rec[b] = int4{E.n, E.hh, E.j, (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
+      P.rec[b] = int4{E.row0 + E.j * P.T, min(P.T, E.S.w - E.j * P.T) * heads_of(P, E.hh % P.parts), E.hh,
+                      (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
     if (!more) break;
     parity ^= 1;
   }
   if (side == 0) end_phase(false);  // as many barriers on both sides
 }
 
-constexpr int kJoinRows = 16;  // rows of a workgroup of the join, 32 lanes each
+constexpr int kJoinThreads = 512;
 
-// Joins the partial results of the unit that begins in range blockIdx.x and ends in another one, for kJoinRows of its rows.
-__global__ __launch_bounds__(kJoinRows * 32) void chunk_join_kernel(const ChunkParams P) {
+// Joins the partial results of the unit that begins in range blockIdx.x and ends in another one, for 16 R of its rows: 32
+// lanes take R of them. Two where a call has many (128 rows over 4K tokens 55 us, 59 with one), one where the parts
+// are what is many (8 rows over 4K 24.4 us, 25.6 with two).
+template <int R>
+__global__ __launch_bounds__(kJoinThreads) void chunk_join_kernel(const ChunkParams P) {
   const int4 rec = P.rec[blockIdx.x];
-  if (rec.x < 0) return;
-  int row0;
-  const ChunkSeq S = seq_of_uniform(P, __builtin_amdgcn_readfirstlane(rec.x), row0);
-  const int g = rec.y / P.parts, hp = rec.y % P.parts, heads = heads_of(P, hp), first = rec.z * P.T;
-  const int x = blockIdx.y * kJoinRows + (threadIdx.x >> 5), t = threadIdx.x & 31;
-  if (x >= min(P.T, S.w - first) * heads) return;
-  const int tok = x / heads;
-  const size_t out = (size_t)(row0 + first + tok) * P.Hq + g * P.G + hp * P.GP + (x - tok * heads);
+  const int x0 = blockIdx.y * (kJoinThreads / 32 * R) + (threadIdx.x >> 5), t = threadIdx.x & 31;
+  if (x0 >= rec.y) return;
+  constexpr int kStep = kJoinThreads / 32;
+  const int last = rec.y - 1;
+  int x[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) x[r] = min(x0 + r * kStep, last);
   const size_t stride = (size_t)P.part_rows * kRowFloats;
   const int n_parts = rec.w - (int)blockIdx.x + 1;
   const auto part = [&](int i) { return P.part + ((size_t)(blockIdx.x + i) * 2 + (i == 0)) * stride; };
-  float M = -INFINITY, L = 0.f;
-  f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+  float M[R], L[R];
+  f32x4_t O[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    M[r] = -INFINITY;
+    L[r] = 0.f;
+    O[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
   // N parts at a time, so that their loads wait side by side: two where there are no more, as in most long calls.
   const auto add = [&](auto nc, int i0) __attribute__((always_inline)) {
     constexpr int N = decltype(nc)::value;
-    float m[N], l[N];
-    f32x4_t o[N];
+    float m[N][R], l[N][R];
+    f32x4_t o[N][R];
 #pragma unroll
     for (int i = 0; i < N; ++i) {  // behind the last part: that one again, without weight
       const float* p = part(min(i0 + i, n_parts - 1));
-      m[i] = p[(size_t)P.part_rows * kHeadDim + x];
-      l[i] = p[(size_t)P.part_rows * (kHeadDim + 1) + x];
-      o[i] = *reinterpret_cast<const f32x4_t*>(p + (size_t)x * kHeadDim + t * 4);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        m[i][r] = p[(size_t)P.part_rows * kHeadDim + x[r]];
+        l[i][r] = p[(size_t)P.part_rows * (kHeadDim + 1) + x[r]];
+        o[i][r] = *reinterpret_cast<const f32x4_t*>(p + (size_t)x[r] * kHeadDim + t * 4);
+      }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (i0 + i >= n_parts) break;
-      const float mx = fmaxf(M, m[i]), base = mx == -INFINITY ? 0.f : mx;
-      const float a = __builtin_amdgcn_exp2f((M - base) * P.scale_log2), c = __builtin_amdgcn_exp2f((m[i] - base) * P.scale_log2);
-      L = a * L + c * l[i];
-      O = a * O + c * o[i];
-      M = mx;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float mx = fmaxf(M[r], m[i][r]), base = mx == -INFINITY ? 0.f : mx;
+        const float a = __builtin_amdgcn_exp2f((M[r] - base) * P.scale_log2);
+        const float c = __builtin_amdgcn_exp2f((m[i][r] - base) * P.scale_log2);
+        L[r] = a * L[r] + c * l[i][r];
+        O[r] = a * O[r] + c * o[i][r];
+        M[r] = mx;
+      }
     }
   };
   if (n_parts <= 2) add(std::integral_constant<int, 2>{}, 0);
   else
     for (int i0 = 0; i0 < n_parts; i0 += 8) add(std::integral_constant<int, 8>{}, i0);
-  const bool none = L == 0.f;
-  float v[4];
+  const int hp = rec.z % P.parts, heads = heads_of(P, hp), head0 = rec.z / P.parts * P.G + hp * P.GP;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : O[e] / L;
-  store4(P.o + out * kHeadDim + t * 4, v);
-  if (P.lse && t == 0) P.lse[out] = none ? -INFINITY : M * P.scale + logf(L);
+  for (int r = 0; r < R; ++r) {
+    if (x0 + r * kStep > last) break;
+    const int tok = x[r] / heads;
+    const size_t out = (size_t)(rec.x + tok) * P.Hq + head0 + (x[r] - tok * heads);
+    const bool none = L[r] == 0.f;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : O[r][e] / L[r];
+    store4(P.o + out * kHeadDim + t * 4, v);
+    if (P.lse && t == 0) P.lse[out] = none ? -INFINITY : M[r] * P.scale + logf(L[r]);
+  }
 }
 
 // Rows of a partial result: those that a unit can have.
@@ -807,7 +830,12 @@ hipError_t launch_chunk_attention(const ChunkShape& sh, const ChunkArgs& a, hipS
     hipLaunchKernelGGL(chunk_kernel<int64_t>, dim3(grid), dim3(kThreads), 0, stream, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(chunk_join_kernel, dim3(grid, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinRows * 32), 0, stream, P);
+  const auto join = [&](auto kernel, int r) {
+    const int per = kJoinThreads / 32 * r;
+    hipLaunchKernelGGL(kernel, dim3(grid, (rows + per - 1) / per), dim3(kJoinThreads), 0, stream, P);
+  };
+  if (rows > 64) join(chunk_join_kernel<2>, 2);
+  else join(chunk_join_kernel<1>, 1);
   return hipGetLastError();
 }
 
