@@ -131,7 +131,7 @@ template <class I>
 struct Unit {
   ChunkSeq S;
   int n, row0;  // sequence, its first row
-  int hh, j;    // KV head and part, unit of these
+  int g, hp, j; // KV head, part of its group, unit of these
   I at;         // its first slot
   int tiles, t0, t1;
 };
@@ -141,8 +141,8 @@ __device__ __forceinline__ void put(int32_t* to, const Unit<I>& u) {
   if ((threadIdx.x & 63) == 0) {
     int4* p = reinterpret_cast<int4*>(to);
     p[0] = int4{u.S.len, u.S.w, u.n, u.row0};
-    p[1] = int4{u.hh, u.j, (int)u.at, (int)((int64_t)u.at >> 32)};
-    p[2] = int4{u.tiles, u.t0, u.t1, 0};
+    p[1] = int4{u.g, u.j, (int)u.at, (int)((int64_t)u.at >> 32)};
+    p[2] = int4{u.tiles, u.t0, u.t1, u.hp};
   }
 }
 template <class I>
@@ -150,7 +150,7 @@ __device__ __forceinline__ Unit<I> get(const int32_t* from, const ChunkParams& P
   asm volatile("" ::: "memory");
   const int4* p = reinterpret_cast<const int4*>(from);
   const int4 a = p[0], b = p[1], c = p[2];
-  return {{uniform(a.x), uniform(a.y), P.T, P.GP}, uniform(a.z), uniform(a.w), uniform(b.x), uniform(b.y),
+  return {{uniform(a.x), uniform(a.y), P.T, P.GP}, uniform(a.z), uniform(a.w), uniform(b.x), uniform(c.w), uniform(b.y),
           uniform((I)((int64_t)(uint32_t)b.z | (int64_t)b.w << 32)), uniform(c.x), uniform(c.y), uniform(c.z)};
 }
 
@@ -264,10 +264,12 @@ void chunk_kernel(const ChunkParams P) {
       return first;
     };
     const I one = uniform(D.S.template slots<I>());
-    D.hh = all_heads == 1 ? 0 : search(all_heads, begin - D.at, [&](int i) { return one * i; });
-    D.at += D.hh * one;
+    const int hh = all_heads == 1 ? 0 : uniform(search(all_heads, begin - D.at, [&](int i) { return one * i; }));
+    D.g = P.parts == 1 ? hh : uniform(hh / P.parts);
+    D.hp = hh - D.g * P.parts;
+    D.at += hh * one;
     const int units = uniform(D.S.units());
-    D.j = units == 1 ? 0 : search(units, begin - D.at, [&](int i) { return D.S.template start<I>(i); });
+    D.j = units == 1 ? 0 : uniform(search(units, begin - D.at, [&](int i) { return D.S.template start<I>(i); }));
     D.at = uniform(D.at + D.S.template start<I>(D.j));
   }
   const auto settle = [&](Unit<I>& u, I begin, I end) __attribute__((always_inline)) {
@@ -282,8 +284,12 @@ void chunk_kernel(const ChunkParams P) {
     if (u.at >= end) return false;
     if (++u.j == u.S.units()) {
       u.j = 0;
-      if (++u.hh == all_heads) {
-        u.hh = 0;
+      if (++u.hp == P.parts) {
+        u.hp = 0;
+        ++u.g;
+      }
+      if (u.g == P.Hkv) {
+        u.g = 0;
         do {  // there are slots left, so there is another sequence with rows
           if (++u.n >= P.B) return false;
           u.S = seq_of_uniform(P, u.n, u.row0);
@@ -314,17 +320,20 @@ void chunk_kernel(const ChunkParams P) {
   const auto fetch_from = [&](const Unit<I>& u) __attribute__((always_inline)) {
     f_keys = uniform(u.S.keys(u.j));
     f_first = u.S.len - u.S.w + u.j * P.T;
-    f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)(P.parts == 1 ? u.hh : u.hh / P.parts) * head_bytes));
+    f_cache = (uint64_t)uniform((int64_t)((uint64_t)(side ? P.vc : P.kc) + (uint64_t)u.g * head_bytes));
     f_row = P.table + (size_t)u.n * P.max_pages;
   };
   // Physical pages of the runs of tiles t .. t + 63, one tile a lane (run r: rows 32 wl + 16 r).
+  // Behind the last key the last entry is read again (no branch in which lanes part: what follows stays uniform).
   const auto look_up = [&](int t) __attribute__((always_inline)) {
+    const int ln = again(lane);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int64_t x = (int64_t)(t + lane) * kTile + wl * 32 + r * 16;
-      int p = 0;
-      if (x < f_keys) p = f_row[x >> P.log2_page];
-      pg[r] = p;
+      pg[r] = 0;
+      if (f_keys > 0) {
+        const int64_t x = (int64_t)(t + ln) * kTile + wl * 32 + r * 16;
+        pg[r] = f_row[min(x, (int64_t)f_keys - 1) >> P.log2_page];
+      }
     }
   };
   const auto copy = [&](int t, int i, int buf) __attribute__((always_inline)) {
@@ -387,8 +396,7 @@ void chunk_kernel(const ChunkParams P) {
 
   // This lane's row of unit u: token and head (behind the unit's last token: that one again, which is not stored).
   const auto row_of = [&](const Unit<I>& u, int x, int& tok, int& head) __attribute__((always_inline)) -> int {
-    const int hp = P.parts == 1 ? 0 : uniform(u.hh % P.parts), g = P.parts == 1 ? u.hh : uniform(u.hh / P.parts);
-    const int heads = heads_of(P, hp), tokens = min(P.T, u.S.w - u.j * P.T);
+    const int heads = heads_of(P, u.hp), tokens = min(P.T, u.S.w - u.j * P.T);
     const int packed = lds.row[x];
     tok = packed >> 16;
     head = packed & 0xffff;
@@ -396,7 +404,7 @@ void chunk_kernel(const ChunkParams P) {
       tok = x / heads;
       head = x - tok * heads;
     }
-    head += g * P.G + hp * P.GP;
+    head += u.g * P.G + u.hp * P.GP;
     const bool real = tok < tokens;
     tok = u.j * P.T + min(tok, tokens - 1);
     return real;
@@ -426,7 +434,7 @@ void chunk_kernel(const ChunkParams P) {
   put(lds.unit[w][0], D);
   for (;;) {
     const Unit<I> D = get<I>(lds.unit[w][parity], P);
-    const bool live = w * 32 < min(P.T, D.S.w - D.j * P.T) * heads_of(P, uniform(D.hh % P.parts));
+    const bool live = w * 32 < min(P.T, D.S.w - D.j * P.T) * heads_of(P, D.hp);
     const int pos_low = uniform(pos);  // of the wave's rows
     const int pos_top = __builtin_amdgcn_readlane(pos, 31);
     f32x16_t o[4];
@@ -592,7 +600,7 @@ void chunk_kernel(const ChunkParams P) {
       int to = t + 1;
       if (last) {
         Unit<I> N = get<I>(lds.unit[w][parity], P);
-        more = advance(N, uniform((I)lds.range[0]), uniform((I)lds.range[1]));
+        more = uniform((int)advance(N, uniform((I)lds.range[0]), uniform((I)lds.range[1])));
         i = 0;
         to = 0;
         if (more) {
@@ -620,110 +628,112 @@ void chunk_kernel(const ChunkParams P) {
       buf ^= 1;
     }
 
+    if (!more && side == 0) end_phase(false);  // as many barriers on both sides; side 1 need not wait for these results
     const Unit<I> E = get<I>(lds.unit[w][parity], P);
-    // Results go to memory in whole rows, through the part of the tile that this wave moves, in the buffer of the unit's last
-    // tile: its K when side 0 is done (side 1 has had it), its V when side 1 is. A row's 16-byte slot s lies at s ^ row % 16.
-    lsum = half_sum(lsum);
     const bool whole = E.t0 == 0 && E.t1 == E.tiles;
-    const int ln = again(lane), hf = ln >> 5, r32 = ln & 31, x = w * 32 + r32;
-    int tok, head;
-    const int real = row_of(E, x, tok, head);
-    char* stage = (side ? lds.v[0] : lds.k[0]) + (buf ^ 1) * kTileBytes + wl * 32 * 256;
-    char* mine_row = stage + r32 * 256;
-    const int n_real = __builtin_popcountll(__ballot(real)) / 2;  // rows of the wave, the first ones
-    const int r4 = ln >> 4, slot = ln & 15;  // of rows 4 i + r4
-    // The values that were taken as 0, to the staged rows that see them: elements d0 .. d0 + n - 1, T each.
-    const auto add_odd = [&](auto type, int d0, int n, bool none) __attribute__((always_inline)) {
-      using V = decltype(type);
-      const int32_t* trow = P.table + (size_t)E.n * P.max_pages;
-      const int to = (int)min((int64_t)E.t1 * kTile, (int64_t)E.S.len) - 1;
+    if (live) {
+      // Results go to memory in whole rows, through the part of the tile that this wave moves, in the buffer of the unit's last
+      // tile: its K when side 0 is done (side 1 has had it), its V when side 1 is. A row's 16-byte slot s lies at s ^ row % 16.
+      lsum = half_sum(lsum);
+      const int ln = again(lane), hf = ln >> 5, r32 = ln & 31, x = w * 32 + r32;
+      int tok, head;
+      const int real = row_of(E, x, tok, head);
+      char* stage = (side ? lds.v[0] : lds.k[0]) + (buf ^ 1) * kTileBytes + wl * 32 * 256;
+      char* mine_row = stage + r32 * 256;
+      const int n_real = __builtin_popcountll(__ballot(real)) / 2;  // rows of the wave, the first ones
+      const int r4 = ln >> 4, slot = ln & 15;  // of rows 4 i + r4
+      // The values that were taken as 0, to the staged rows that see them: elements d0 .. d0 + n - 1, T each.
+      const auto add_odd = [&](auto type, int d0, int n, bool none) __attribute__((always_inline)) {
+        using V = decltype(type);
+        const int32_t* trow = P.table + (size_t)E.n * P.max_pages;
+        const int to = (int)min((int64_t)E.t1 * kTile, (int64_t)E.S.len) - 1;
 #pragma unroll 1
-      for (int t = odd_from; t <= to; ++t) {
-        const int32_t e = ld_uniform(trow + (t >> P.log2_page));
-        const uint64_t p = (uint32_t)e < (uint64_t)P.n_pages ? (uint32_t)e : 0u;
-        const uint16_t* v = P.vc + (p * page_bytes + (uint64_t)uniform(E.hh / P.parts) * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim;
+        for (int t = odd_from; t <= to; ++t) {
+          const int32_t e = ld_uniform(trow + (t >> P.log2_page));
+          const uint64_t p = (uint32_t)e < (uint64_t)P.n_pages ? (uint32_t)e : 0u;
+          const uint16_t* v = P.vc + (p * page_bytes + (uint64_t)E.g * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim;
 #pragma unroll 1
-        for (int i = hf * (n / 2); i < (hf + 1) * (n / 2); ++i) {
-          const uint32_t bits = (uint32_t)v[d0 + i] << 16;
-          if ((bits & 0x7f800000u) != 0x7f800000u || t > E.S.len - E.S.w + tok || none) continue;
-          const int byte = i * (int)sizeof(V);
-          V* x = reinterpret_cast<V*>(mine_row + (((byte >> 4) ^ (r32 & 15)) << 4) + (byte & 15));
-          *x = (V)((float)*x + __uint_as_float(bits));
+          for (int i = hf * (n / 2); i < (hf + 1) * (n / 2); ++i) {
+            const uint32_t bits = (uint32_t)v[d0 + i] << 16;
+            if ((bits & 0x7f800000u) != 0x7f800000u || t > E.S.len - E.S.w + tok || none) continue;
+            const int byte = i * (int)sizeof(V);
+            V* x = reinterpret_cast<V*>(mine_row + (((byte >> 4) ^ (r32 & 15)) << 4) + (byte & 15));
+            *x = (V)((float)*x + __uint_as_float(bits));
+          }
         }
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    };
-    if (!whole) {
-      float* part = P.part + ((size_t)b * 2 + (E.t0 == 0)) * P.part_rows * kRowFloats;
-      const float by = far || m == -INFINITY ? 1.f : exact_by(m, P.scale_log2);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      };
+      if (!whole) {
+        float* part = P.part + ((size_t)b * 2 + (E.t0 == 0)) * P.part_rows * kRowFloats;
+        const float by = far || m == -INFINITY ? 1.f : exact_by(m, P.scale_log2);
 #pragma unroll
-      for (int hd = 0; hd < 2; ++hd) {
+        for (int hd = 0; hd < 2; ++hd) {
+#pragma unroll
+          for (int z = 0; z < 8; ++z) {
+            const int dt = 2 * hd + (z >> 2), rg = z & 3;
+            *reinterpret_cast<f32x4_t*>(mine_row + (((2 * z + hf) ^ (r32 & 15)) << 4)) =
+                by * f32x4_t{o[dt][4 * rg], o[dt][4 * rg + 1], o[dt][4 * rg + 2], o[dt][4 * rg + 3]};
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (odd_from != INT_MAX) add_odd(0.f, 64 * hd, 64, false);
+          f32x4_t v[8];
+#pragma unroll
+          for (int z = 0; z < 8; ++z)
+            v[z] = *reinterpret_cast<const f32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
+#pragma unroll
+          for (int z = 0; z < 8; ++z)
+            if (4 * z + r4 < n_real)
+              *reinterpret_cast<f32x4_t*>(part + (size_t)(w * 32 + 4 * z + r4) * kHeadDim + 64 * hd + 4 * slot) = v[z];
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        if (hf == 0 && real) {
+          part[(size_t)P.part_rows * kHeadDim + x] = m;
+          part[(size_t)P.part_rows * (kHeadDim + 1) + x] = by * lsum;
+        }
+      } else {
+        // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
+        const bool none = lsum == 0.f;
+        const float inv = none ? 0.f : 1.f / lsum;
+        if (__any(none)) {
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[dt][r] = none ? 0.f : o[dt][r];
+        }
+        const int out = (E.row0 + tok) * P.Hq + head;
+#pragma unroll
+        for (int z = 0; z < 16; ++z) {
+          const int dt = z >> 2, rg = z & 3;
+          uint32_t two[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const __bf16 lo = (__bf16)(o[dt][4 * rg + 2 * e] * inv), hi = (__bf16)(o[dt][4 * rg + 2 * e + 1] * inv);
+            two[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
+          }
+          *reinterpret_cast<u32x2_t*>(mine_row + ((z ^ (r32 & 15)) << 4) + 8 * hf) = u32x2_t{two[0], two[1]};
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (odd_from != INT_MAX) add_odd((__bf16)0.f, 0, kHeadDim, none);
+        u32x4_t v[8];
+        int to[8];
 #pragma unroll
         for (int z = 0; z < 8; ++z) {
-          const int dt = 2 * hd + (z >> 2), rg = z & 3;
-          *reinterpret_cast<f32x4_t*>(mine_row + (((2 * z + hf) ^ (r32 & 15)) << 4)) =
-              by * f32x4_t{o[dt][4 * rg], o[dt][4 * rg + 1], o[dt][4 * rg + 2], o[dt][4 * rg + 3]};
+          v[z] = *reinterpret_cast<const u32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
+          to[z] = __shfl(out, 4 * z + r4, 64);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (odd_from != INT_MAX) add_odd(0.f, 64 * hd, 64, false);
-        f32x4_t v[8];
 #pragma unroll
         for (int z = 0; z < 8; ++z)
-          v[z] = *reinterpret_cast<const f32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
-#pragma unroll
-        for (int z = 0; z < 8; ++z)
-          if (4 * z + r4 < n_real)
-            *reinterpret_cast<f32x4_t*>(part + (size_t)(w * 32 + 4 * z + r4) * kHeadDim + 64 * hd + 4 * slot) = v[z];
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (4 * z + r4 < n_real) *reinterpret_cast<u32x4_t*>(P.o + (size_t)to[z] * kHeadDim + slot * 8) = v[z];
+        if (P.lse && hf == 0 && real) P.lse[out] = none ? -INFINITY : (far ? m * P.scale : rounded(m, P.scale_log2) * kLn2) + logf(lsum);
       }
-      if (hf == 0 && real) {
-        part[(size_t)P.part_rows * kHeadDim + x] = m;
-        part[(size_t)P.part_rows * (kHeadDim + 1) + x] = by * lsum;
-      }
-    } else {
-      // nothing to attend to: 0 (a sum that is NaN, from a NaN logit, stays NaN)
-      const bool none = lsum == 0.f;
-      const float inv = none ? 0.f : 1.f / lsum;
-      if (__any(none)) {
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[dt][r] = none ? 0.f : o[dt][r];
-      }
-      const int out = (E.row0 + tok) * P.Hq + head;
-#pragma unroll
-      for (int z = 0; z < 16; ++z) {
-        const int dt = z >> 2, rg = z & 3;
-        uint32_t two[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const __bf16 lo = (__bf16)(o[dt][4 * rg + 2 * e] * inv), hi = (__bf16)(o[dt][4 * rg + 2 * e + 1] * inv);
-          two[e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
-        }
-        *reinterpret_cast<u32x2_t*>(mine_row + ((z ^ (r32 & 15)) << 4) + 8 * hf) = u32x2_t{two[0], two[1]};
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (odd_from != INT_MAX) add_odd((__bf16)0.f, 0, kHeadDim, none);
-      u32x4_t v[8];
-      int to[8];
-#pragma unroll
-      for (int z = 0; z < 8; ++z) {
-        v[z] = *reinterpret_cast<const u32x4_t*>(stage + (4 * z + r4) * 256 + ((slot ^ ((4 * z + r4) & 15)) << 4));
-        to[z] = __shfl(out, 4 * z + r4, 64);
-      }
-#pragma unroll
-      for (int z = 0; z < 8; ++z)
-        if (4 * z + r4 < n_real) *reinterpret_cast<u32x4_t*>(P.o + (size_t)to[z] * kHeadDim + slot * 8) = v[z];
-      if (P.lse && hf == 0 && real) P.lse[out] = none ? -INFINITY : (far ? m * P.scale : rounded(m, P.scale_log2) * kLn2) + logf(lsum);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     if (threadIdx.x == 0 && E.t0 == 0 && !whole)
-      P.rec[b] = int4{E.row0 + E.j * P.T, min(P.T, E.S.w - E.j * P.T) * heads_of(P, E.hh % P.parts), E.hh,
+      P.rec[b] = int4{E.row0 + E.j * P.T, min(P.T, E.S.w - E.j * P.T) * heads_of(P, E.hp), E.g * P.parts + E.hp,
                       (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
     if (!more) break;
     parity ^= 1;
   }
-  if (side == 0) end_phase(false);  // as many barriers on both sides
 }
 
 constexpr int kJoinThreads = 512;
