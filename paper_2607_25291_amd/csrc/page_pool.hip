@@ -5,7 +5,10 @@
 // the marks as bits in LDS. Otherwise kernels one after the other, with the marks as bytes in the workspace (plain
 // stores: a page marked twice gets the same byte twice): clear, mark, count by blocks, write.
 //
-// Bound: the launches' latency; the tables once (4 bytes an entry), the marks.
+// Bound: few entries, latency (64 rows: release 6.4 us, compaction 11.6, of which the second walk over the table and its
+// dependent loads are half). Many: the marks' stores, one byte each at random places (591K entries of 512 rows: 10.5 of
+// release's 19 us; 559K: 11 of compaction's 34), then launches that wait for each other, 2 to 4 us each, and the
+// compaction's lists and tables, 8 and 12 us.
 #include <algorithm>
 
 #include "cosa_device.h"
@@ -91,14 +94,6 @@ __device__ __forceinline__ void for_pages(const int32_t* row, int from, int step
   }
 }
 
-// f(page) for the pages that workgroup turn x of a table holds: kEntries entries of one row.
-template <class F>
-__device__ __forceinline__ void for_held(const int32_t* table, const int32_t* lens, int max_pages, int log2_page,
-                                         long long n_pages, int x, F&& f) {
-  const int turns = (max_pages + kEntries - 1) / kEntries, row = x / turns, j0 = x % turns * kEntries;
-  const int j1 = min(j0 + kEntries, held_pages(lens[row], max_pages, log2_page));
-  for_pages(table + (size_t)row * max_pages, j0 + (int)threadIdx.x, kThreads, j1, n_pages, [&](int, int p) { f(p); });
-}
 
 // ---- release
 
@@ -107,14 +102,34 @@ __device__ __forceinline__ void free_list(const PageReleaseArgs& A, int& taken, 
   taken = A.n_taken ? min(max(*A.n_taken, 0), n_free) : 0;
 }
 
-// marks: pages that are held afterwards or listed already; marks2: pages that were held.
-__global__ __launch_bounds__(kThreads) void release_mark_kernel(PageReleaseArgs A, Pool W, int old_turns, int new_turns) {
-  const int all = old_turns + new_turns;
-  for (int x = blockIdx.x; x < all; x += gridDim.x) {
-    if (x < old_turns)
-      for_held(A.old_table, A.old_lens, A.max_pages, A.log2_page, A.n_pages, x, [&](int p) { W.marks2[p] = 1; });
-    else
-      for_held(A.new_table, A.new_lens, A.max_pages, A.log2_page, A.n_pages, x - old_turns, [&](int p) { W.marks[p] = 1; });
+// The rows of both tables, or of the one that both are, whose entries are then read and marked once (512 rows, of which half
+// end, 18.9 us, as two tables 23.5).
+struct ReleaseRow {
+  const int32_t* entries;
+  int was, is;  // entries held before and afterwards; 0 for a row that the other table has
+};
+__host__ __device__ __forceinline__ bool one_table(const PageReleaseArgs& A) {
+  return A.old_table == A.new_table && A.old_batch == A.new_batch;
+}
+__host__ __device__ __forceinline__ int release_rows(const PageReleaseArgs& A) {
+  return one_table(A) ? A.old_batch : A.old_batch + A.new_batch;
+}
+__device__ __forceinline__ ReleaseRow release_row(const PageReleaseArgs& A, int row) {
+  const bool old = row < A.old_batch;
+  const int y = old ? row : row - A.old_batch;
+  return {(old ? A.old_table : A.new_table) + (size_t)y * A.max_pages,
+          old ? held_pages(A.old_lens[y], A.max_pages, A.log2_page) : 0,
+          !old || one_table(A) ? held_pages(A.new_lens[y], A.max_pages, A.log2_page) : 0};
+}
+
+// marks: pages that are held afterwards or listed already; marks2: pages that were held, but for those.
+__global__ __launch_bounds__(kThreads) void release_mark_kernel(PageReleaseArgs A, Pool W, int turns) {
+  const int per_row = (A.max_pages + kEntries - 1) / kEntries;
+  for (int x = blockIdx.x; x < turns; x += gridDim.x) {
+    const ReleaseRow R = release_row(A, x / per_row);
+    const int j0 = x % per_row * kEntries;
+    for_pages(R.entries, j0 + (int)threadIdx.x, kThreads, min(j0 + kEntries, max(R.was, R.is)), A.n_pages,
+              [&](int j, int p) { (j < R.is ? W.marks : W.marks2)[p] = 1; });
   }
   int taken, n_free;
   free_list(A, taken, n_free);
@@ -199,8 +214,13 @@ __device__ __forceinline__ void plan_page(const PageCompactArgs& A, const Plan& 
 }
 
 __global__ __launch_bounds__(kThreads) void compact_mark_kernel(PageCompactArgs A, Pool W, int turns) {
-  for (int x = blockIdx.x; x < turns; x += gridDim.x)
-    for_held(A.table, A.seq_lens, A.max_pages, A.log2_page, A.n_pages, x, [&](int p) { W.marks[p] = 1; });
+  const int per_row = (A.max_pages + kEntries - 1) / kEntries;
+  for (int x = blockIdx.x; x < turns; x += gridDim.x) {
+    const int row = x / per_row, j0 = x % per_row * kEntries;
+    const int j1 = min(j0 + kEntries, held_pages(A.seq_lens[row], A.max_pages, A.log2_page));
+    for_pages(A.table + (size_t)row * A.max_pages, j0 + (int)threadIdx.x, kThreads, j1, A.n_pages,
+              [&](int, int p) { W.marks[p] = 1; });
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void compact_plan_kernel(PageCompactArgs A, Pool W) {
@@ -280,16 +300,6 @@ constexpr int kOneThreads = 1024;
 constexpr int kOneWords = 4096;                // words of marks in LDS
 constexpr long long kOnePages = kOneWords * 32;
 
-template <class F>
-__device__ __forceinline__ void one_for_held(const int32_t* table, const int32_t* lens, int batch, int max_pages, int log2_page,
-                                             long long n_pages, F&& f) {
-  const int lane = threadIdx.x & 63;
-  for (int row = threadIdx.x >> 6; row < batch; row += kOneThreads / 64) {
-    const int held = held_pages(lens[row], max_pages, log2_page);
-    for_pages(table + (size_t)row * max_pages, lane, 64, held, n_pages, [&](int, int p) { f(p); });
-  }
-}
-
 __global__ __launch_bounds__(kOneThreads) void release_one_kernel(PageReleaseArgs A) {
   __shared__ uint32_t now[kOneWords], before[kOneWords], waves[kOneThreads / 64];
   const int words = (int)((A.n_pages + 31) / 32);
@@ -297,10 +307,12 @@ __global__ __launch_bounds__(kOneThreads) void release_one_kernel(PageReleaseArg
   int taken, n_free;
   free_list(A, taken, n_free);
   __syncthreads();
-  one_for_held(A.old_table, A.old_lens, A.old_batch, A.max_pages, A.log2_page, A.n_pages,
-               [&](int p) { atomicOr(&before[p >> 5], 1u << (p & 31)); });
-  one_for_held(A.new_table, A.new_lens, A.new_batch, A.max_pages, A.log2_page, A.n_pages,
-               [&](int p) { atomicOr(&now[p >> 5], 1u << (p & 31)); });
+  const int rows = release_rows(A);
+  for (int row = threadIdx.x >> 6; row < rows; row += kOneThreads / 64) {
+    const ReleaseRow R = release_row(A, row);
+    for_pages(R.entries, threadIdx.x & 63, 64, max(R.was, R.is), A.n_pages,
+              [&](int j, int p) { atomicOr((j < R.is ? now : before) + (p >> 5), 1u << (p & 31)); });
+  }
   for (int i = taken + (int)threadIdx.x; i < n_free; i += kOneThreads) {
     const int p = A.free_pages[i];
     if (p >= 0 && p < A.n_pages) atomicOr(&now[p >> 5], 1u << (p & 31));
@@ -322,8 +334,10 @@ __global__ __launch_bounds__(kOneThreads) void compact_one_kernel(PageCompactArg
   const int words = (int)((A.n_pages + 31) / 32);
   for (int i = threadIdx.x; i < words; i += kOneThreads) marks[i] = 0u;
   __syncthreads();
-  one_for_held(A.table, A.seq_lens, A.batch, A.max_pages, A.log2_page, A.n_pages,
-               [&](int p) { atomicOr(&marks[p >> 5], 1u << (p & 31)); });
+  for (int row = threadIdx.x >> 6; row < A.batch; row += kOneThreads / 64)
+    for_pages(A.table + (size_t)row * A.max_pages, threadIdx.x & 63, 64,
+              held_pages(A.seq_lens[row], A.max_pages, A.log2_page), A.n_pages,
+              [&](int, int p) { atomicOr(&marks[p >> 5], 1u << (p & 31)); });
   __syncthreads();
   const int per = (words + kOneThreads - 1) / kOneThreads, w0 = min((int)threadIdx.x * per, words), w1 = min(w0 + per, words);
   uint32_t mine = 0, total;
@@ -378,7 +392,7 @@ void clear(void* p, size_t bytes, hipStream_t stream) {
 }
 
 // One workgroup where the tables' entries are few: it is bound by its instructions, the kernels by their launches. Release of
-// 40K / 80K entries 6.9 / 11.0 us with one workgroup, 16.6 / 15.7 with kernels; compaction of 10K / 20K / 40K / 80K
+// 40K / 80K entries 6.9 / 9.0 us with one workgroup, with kernels (over two tables) 16.6 / 15.7; compaction of 10K / 20K / 40K / 80K
 // entries 7.1 / 12.0 / 20.7 / 38 and 17 to 20.
 constexpr long long kOneRelease = 1 << 17, kOneCompact = 1 << 15;
 
@@ -387,16 +401,16 @@ constexpr long long kOneRelease = 1 << 17, kOneCompact = 1 << 15;
 size_t page_workspace_bytes(long long n_pages) { return Pool(nullptr, n_pages).bytes; }
 
 hipError_t launch_page_release(const PageReleaseArgs& a, hipStream_t stream) {
-  if (a.n_pages <= kOnePages && ((long long)a.old_batch + a.new_batch) * a.max_pages + a.free_capacity <= kOneRelease) {
+  if (a.n_pages <= kOnePages && (long long)release_rows(a) * a.max_pages + a.free_capacity <= kOneRelease) {
     hipLaunchKernelGGL(release_one_kernel, dim3(1), dim3(kOneThreads), 0, stream, a);
     return hipGetLastError();
   }
   const Pool W(a.workspace, a.n_pages);
   clear(W.marks, 2 * (size_t)W.blocks * kBlockPages, stream);
-  const int old_turns = turns_of(a.old_batch, a.max_pages), new_turns = turns_of(a.new_batch, a.max_pages);
+  const int turns = turns_of(release_rows(a), a.max_pages);
   const long long lists = ((long long)a.free_capacity + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(release_mark_kernel, dim3(grid_of(std::max<long long>((long long)old_turns + new_turns, lists), 2048)),
-                     dim3(kThreads), 0, stream, a, W, old_turns, new_turns);
+  hipLaunchKernelGGL(release_mark_kernel, dim3(grid_of(std::max<long long>(turns, lists), 2048)), dim3(kThreads), 0, stream, a,
+                     W, turns);
   hipLaunchKernelGGL((count_kernel<true>), dim3(W.blocks), dim3(kThreads), 0, stream, W);
   hipLaunchKernelGGL(release_write_kernel, dim3(W.blocks), dim3(kThreads), 0, stream, a, W);
   return hipGetLastError();

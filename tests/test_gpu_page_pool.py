@@ -230,3 +230,20 @@ def test_compact_edges():
     whole = Rows(rng, [16 * 4096], 16, spare=0)  # everything in use, whole blocks
     compact(whole)
     compact(Rows(rng, [], 16, width=2), n_pages=5)
+
+
+@pytest.mark.parametrize("rows,longest", [(40, 900), (200, 14000)])
+def test_release_from_one_table_and_from_two(rows, longest):
+    """One table is read once, whichever length is the larger one; rows share pages, also within themselves."""
+    rng = np.random.default_rng(rows)
+    t = Rows(rng, lengths(rng, rows, longest, 16), 16, spare=50)
+    table = t.table.copy()
+    behind = np.arange(t.width)[None] >= -(-t.lens // 16)[:, None]
+    table[behind] = rng.integers(0, t.n_pages, behind.sum())
+    cap = t.width * 16
+    pick = rng.integers(0, 4, rows)
+    new = np.choose(pick, [np.zeros(rows, int), t.lens // 3, t.lens, np.minimum(t.lens + rng.integers(1, 500, rows), cap)])
+    free = t.free[:30]
+    one = release((table, t.lens), (table, new), 16, t.n_pages, free, len(free), 3)
+    two = release((table, t.lens), (table.copy(), new), 16, t.n_pages, free, len(free), 3)
+    assert np.array_equal(one, two)
