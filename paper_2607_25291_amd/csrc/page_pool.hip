@@ -392,9 +392,9 @@ void clear(void* p, size_t bytes, hipStream_t stream) {
 }
 
 // One workgroup where the tables' entries are few: it is bound by its instructions, the kernels by their launches. Release of
-// 40K / 80K entries 6.9 / 9.0 us with one workgroup, with kernels (over two tables) 16.6 / 15.7; compaction of 10K / 20K / 40K / 80K
-// entries 7.1 / 12.0 / 20.7 / 38 and 17 to 20.
-constexpr long long kOneRelease = 1 << 17, kOneCompact = 1 << 15;
+// 40K / 80K / 120K entries 8.9 / 14.4 / 20.7 us with one workgroup, 14 to 17 with kernels (box to box); compaction of 10K / 20K /
+// 40K / 80K entries 7.1 / 12.0 / 20.7 / 38 and 17 to 20.
+constexpr long long kOneRelease = 3 << 15, kOneCompact = 1 << 15;
 
 }  // namespace
 
