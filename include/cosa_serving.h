@@ -109,7 +109,8 @@ size_t cosa_page_workspace_bytes(int64_t n_pages);
  * The free list after a step: pages that some row of old_table [old_batch, max_pages] holds with old_lens and no row
  * of new_table [new_batch, max_pages] with new_lens become free. The tables may be the same one: requests that
  * end have new length 0, drafted tokens that are turned down a smaller one; after a fork they are the two
- * tables. free_out int32 [out_capacity] gets
+ * tables. old_lens count the new tokens (cosa_page_map's seq_lens): a page that was taken for tokens which neither
+ * length counts would be lost. free_out int32 [out_capacity] gets
  *   the entries n_taken .. n_free - 1 of free_pages [free_capacity] (n_taken: what cosa_page_map or cosa_page_fork took
  *   from its front, device int32 [1], NULL for 0, read as clamped to [0, n_free]), then
  *   the pages that become free, in ascending order, but for those that are among these entries already;
