@@ -32,7 +32,8 @@ extern "C" {
 
 /* New tokens of a batch of sequences, packed one sequence behind the other. Limits as in cosa_decode.h: head_dim == 128,
  * page_size a power of two in [16, 2^20], max_pages * page_size < 2^31; batch and n_rows below 2^22,
- * n_rows * n_q_heads below 2^31 (COSA_ERR_UNSUPPORTED otherwise). */
+ * n_rows * n_q_heads below 2^31, and, roughly, 3 * batch * n_rows * n_q_heads * max_pages * page_size below 2^70
+ * (COSA_ERR_UNSUPPORTED otherwise). */
 typedef struct {
   int32_t batch;      /* B >= 0                                                                   */
   int32_t n_q_heads;  /* Hq, a multiple of n_kv_heads; query head h reads KV head h / (Hq / Hkv)   */

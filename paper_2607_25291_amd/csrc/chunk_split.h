@@ -75,6 +75,11 @@ constexpr bool chunk_narrow(int64_t batch, int64_t n_rows, int64_t cap, int64_t 
          (double)units * (double)most * kFullSlots * (double)heads * (double)batch < limit / 2;
 }
 
+// Whether 62 bits hold them, whatever the offsets say. Calls of which they do not are refused.
+constexpr bool chunk_fits(int64_t batch, int64_t n_rows, int64_t cap, int64_t heads, int T) {
+  return (double)(n_rows / T + 1) * (double)(cap + kUnitKeys) * kFullSlots * (double)heads * (double)batch < 4611686018427387904.0;
+}
+
 // The ranges of a line of `total` slots: 2^log2_most of `length` slots each; the last ones may have fewer, or none.
 template <class I>
 constexpr I chunk_range(I total, int log2_most, int shortest) {

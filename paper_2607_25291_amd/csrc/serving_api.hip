@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include "api_checks.h"
+#include "chunk_split.h"
 #include "cosa_serving.h"
 #include "serving_internal.h"
 
@@ -53,6 +54,9 @@ cosa_status check_chunk(const cosa_chunk_problem* p, int page_size, ChunkShape& 
   sh.q_stride = p->q_stride ? p->q_stride : dense;
   sh.n_pages = 1;
   sh.scale = p->sm_scale > 0.f ? p->sm_scale : (float)(1.0 / sqrt((double)p->head_dim));
+  if (!cosa::chunk_fits(sh.B, sh.n_rows, sh.cap(), (int64_t)sh.Hkv * cosa::chunk_parts(sh.G), cosa::chunk_tokens(sh.G)))
+    return fail(COSA_ERR_UNSUPPORTED, "%d sequences of up to %d tokens and %d rows: too large for one launch", sh.B, sh.cap(),
+                sh.n_rows);
   empty = p->batch == 0 || p->n_rows == 0;
   return ok();
 }

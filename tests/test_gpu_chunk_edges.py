@@ -255,3 +255,61 @@ def test_captured_and_replayed():
             B.cosa_chunk_attention(p, q[i], kv, lens, cu, ws2, n, o[2], ls[2])
             t.cuda.synchronize()
             assert t.equal(o[i], o[2]) and t.equal(ls[i], ls[2]), (step, i)
+
+
+@pytest.mark.parametrize("batch", [63, 64, 65, 512, 513])
+def test_batches_around_the_lanes_and_threads(batch):
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(0, 90, batch)
+    new = np.where(rng.random(batch) < 0.5, np.minimum(lens, 1), rng.integers(0, 20, batch))
+    new[0], new[-1] = 0, 7
+    c = Cache(rng, lens, 2, 16)
+    q = normal(rng, int(new.sum()), 6, 128)
+    cu = offsets(new)
+    say("[batch]", batch)
+    o, ls = run_chunk(B.ChunkProblem(batch, 6, 2, c.width, q.shape[0]), c, dev(q), dev(cu))
+    check_chunk(*host(o, ls), S.chunk_attention(q, c.k, c.v, c.table, lens, cu), 90)
+
+
+def test_groups_over_several_units_of_several_kv_heads():
+    rng = np.random.default_rng(42)
+    c = Cache(rng, [300, 5], 2, 16)
+    q, cu = normal(rng, 6, 1200, 128), offsets([5, 1])
+    o, ls = run_chunk(B.ChunkProblem(2, 1200, 2, c.width, 6), c, dev(q), dev(cu))
+    check_chunk(*host(o, ls), S.chunk_attention(q, c.k, c.v, c.table, [300, 5], cu), 300)
+
+
+def test_pages_that_rows_share():
+    """Forked sequences, and a page that one row holds twice."""
+    rng = np.random.default_rng(43)
+    c = Cache(rng, [200, 180, 0, 96], 2, 32)
+    c.table[1, :5] = c.table[0, :5]
+    c.table[2, :4], c.lens[2] = c.table[0, :4], 128
+    c.table[3, 2] = c.table[3, 0]
+    new = [40, 20, 128, 96]
+    q, cu = normal(rng, sum(new), 4, 128), offsets(new)
+    o, ls = run_chunk(B.ChunkProblem(4, 4, 2, c.width, sum(new)), c, dev(q), dev(cu))
+    check_chunk(*host(o, ls), S.chunk_attention(q, c.k, c.v, c.table, c.lens, cu), 200)
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace and outputs."""
+    t = torch()
+    rng = np.random.default_rng(44)
+    c = Cache(rng, [4000, 900, 1, 333], 2, 16)
+    kv = c.upload()
+    streams = [t.cuda.Stream() for _ in range(2)]
+    calls = []
+    for new in ([500, 30, 1, 100], [1, 1, 1, 1]):
+        p = B.ChunkProblem(4, 8, 2, c.width, sum(new))
+        q, cu = dev(normal(rng, sum(new), 8, 128)), dev(offsets(new))
+        n = B.cosa_chunk_workspace_bytes(p)
+        calls.append((p, q, cu, run_chunk(p, c, q, cu, kv=kv), t.empty(n, dtype=t.uint8, device="cuda"), n,
+                      t.zeros(sum(new), 8, 128, dtype=t.int16, device="cuda"), t.zeros(sum(new), 8, device="cuda")))
+    t.cuda.synchronize()
+    for _ in range(5):
+        for s, (p, q, cu, _, ws, n, o, ls) in zip(streams, calls):
+            B.cosa_chunk_attention(p, q, kv, c.lens_d, cu, ws, n, o, ls, stream=s)
+    t.cuda.synchronize()
+    for *_, want, ws, n, o, ls in calls:
+        assert t.equal(o, want[0]) and t.equal(ls, want[1])

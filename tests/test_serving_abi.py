@@ -55,6 +55,7 @@ def test_symbols():
     (change(batch=1 << 22), B.COSA_ERR_UNSUPPORTED),
     (change(n_rows=1 << 22), B.COSA_ERR_UNSUPPORTED),
     (change(n_q_heads=2 ** 12, n_rows=2 ** 19), B.COSA_ERR_UNSUPPORTED),
+    (change(batch=2 ** 22 - 1, n_rows=2 ** 22 - 1, max_pages=2 ** 24), B.COSA_ERR_UNSUPPORTED),  # offsets could ask for 2^62 slots
 ])
 def test_chunk_problems(problem, status):
     refused(status, chunk, problem)
