@@ -247,3 +247,40 @@ def test_release_from_one_table_and_from_two(rows, longest):
     one = release((table, t.lens), (table, new), 16, t.n_pages, free, len(free), 3)
     two = release((table, t.lens), (table.copy(), new), 16, t.n_pages, free, len(free), 3)
     assert np.array_equal(one, two)
+
+
+def test_the_largest_pool():
+    """Page numbers up to 2^28, lists shorter than what there is."""
+    t, n_pages, cap = torch(), 1 << 28, 3000
+    table = np.array([[n_pages - 1, 5, n_pages - 1 - 4096], [1 << 27, 0, 77], [n_pages // 3, 2, 1]], np.int32)
+    lens = np.array([48, 33, 10], np.int32)
+    used = {n_pages - 1, 5, n_pages - 1 - 4096, 1 << 27, 0, 77, n_pages // 3}
+    n_ws = B.cosa_page_workspace_bytes(n_pages)
+    ws = t.full((n_ws,), 0xFF, dtype=t.uint8, device="cuda")
+    new, src, dst, n_moves, free, n_free = marked(3, 3), marked(4), marked(4), marked(1), marked(cap), marked(1)
+    say("[largest]")
+    B.cosa_page_compact(3, 16, 3, n_pages, i32(table), i32(lens), 4, new, src, dst, n_moves, free, cap, n_free, ws, n_ws)
+    moves = list(zip(sorted(used)[:-5:-1], [1, 2, 3, 4]))
+    assert list(zip(src.tolist(), dst.tolist())) == moves and n_moves.item() == 4
+    to = dict(moves)
+    want = [[to.get(int(p), int(p)) if j < -(-int(n) // 16) else int(p) for j, p in enumerate(row)] for row, n in zip(table, lens)]
+    assert new.tolist() == want
+    now = {to.get(p, p) for p in used}
+    assert n_free.item() == cap and free.tolist() == [p for p in range(cap + 10) if p not in now][:cap]
+    out, n_out = marked(9), marked(1)
+    B.cosa_page_release(16, 3, n_pages, 3, i32(table), i32(lens), 1, i32(table[:1]), i32(lens[:1]), i32([n_pages - 2]), 1, i32([1]),
+                        None, out, 9, n_out, ws, n_ws)
+    assert n_out.item() == 5 and out.tolist() == [n_pages - 2, 0, 77, n_pages // 3, 1 << 27] + [MARK] * 4
+
+
+def test_copy_behind_4_gib():
+    t, n_pages, hkv, page = torch(), 20000, 4, 256
+    k, v = (t.zeros((n_pages, hkv, page, 128), dtype=t.int16, device="cuda") for _ in range(2))
+    for i, p in enumerate((19999, 3, 17001)):
+        k[p], v[p] = i + 1, -i - 1
+    say("[copy]", "4 GiB")
+    B.cosa_page_copy(hkv, 128, page, n_pages, k, v, None, i32([19999, 3, 17001]), i32([18000, 19000, 0]), i32([256, 9, 100]), 3, i32([3]))
+    for i, (d, keep) in enumerate(((18000, 256), (19000, 9), (0, 100))):
+        for x, sign in ((k, 1), (v, -1)):
+            assert (x[d, :, :keep] == sign * (i + 1)).all() and (x[d, :, keep:] == 0).all()
+    assert (k.view(-1, hkv * page * 128)[:, 0] != 0).sum().item() == 6
