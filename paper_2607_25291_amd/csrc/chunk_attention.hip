@@ -17,11 +17,11 @@
 // their sum takes them with 24 bits): the further bits would be products of their own, and MFMA is what bounds large units.
 //
 // Bound: MFMA, 4 d flops a key and row. 4096 tokens over 64K, 32 / 8 heads: 3.8 to 3.9 ms, 1.10 PFLOP/s of 1.23 in a library
-// matrix product of 8192 rows; 0.57 of the cycles multiply at 1.77 GHz, LDS bank conflicts are below 0.1 %. 256 rows, since
-// a tile of K and V read from LDS by 32 rows a wave then feeds 32 MFMAs a wave, and two waves a SIMD, one phase apart, let
-// one multiply while the other one takes exponentials. What a unit costs beside its tiles (3.5 tiles: Q, edges, results)
-// leaves 840 TFLOP/s in prompts of up to 4K tokens. Units of few rows read K and V at up to 5.8 TB/s (64 sequences of up to
-// 64K tokens and one new token 285 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 us) are two launches and latency.
+// matrix product of 8192 rows; 0.57 of the cycles multiply at 1.77 GHz, LDS bank conflicts are below 0.1 %. 256 rows: eight
+// waves share a tile's copies, and two waves a SIMD, one phase apart, let one multiply while the other one takes
+// exponentials. What a unit costs beside its tiles (3.5 tiles: Q, edges, results) leaves 840 TFLOP/s in prompts of up to 4K
+// tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64 sequences of up to 64K tokens and one new
+// token 287 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 us) are two launches and latency.
 #include <float.h>
 #include <limits.h>
 
