@@ -40,8 +40,8 @@ constexpr int kTile = kChunkTile;
 constexpr int kKeyTiles = kTile / 32;
 constexpr int kTileBytes = kTile * kHeadDim * 2;  // one tensor's
 constexpr int kLog2Grid = 8, kGrid = 1 << kLog2Grid;  // workgroups that share the line: one a CU
-// Slots of the shortest range: at least a tile's. Shorter ones end sooner and leave more to join: 384 / 512 / 768 slots 18.8 /
-// 18.5 / 19.7 us for 8 sequences of up to 1.5K tokens and 2 new ones, 27.9 / 24.9 / 24.4 for 8 rows over 4K tokens.
+// Slots of the shortest range: at least a tile's. Shorter ones end sooner and leave more to join: 384 / 512 slots 17.8 / 18.8 us
+// for 8 rows over 4K tokens, 16.2 / 15.9 for 16 over 1000 and 26.3 / 24.0 for 2 rows of 20 heads over 49K.
 constexpr int kShortest = 512;
 static_assert(kShortest >= kTile * kFullSlots, "every range but the last holds the start of a tile");
 constexpr int kRowFloats = kHeadDim + 2;          // of a partial result: O, maximum, sum
@@ -51,7 +51,9 @@ struct ChunkParams {
   const uint16_t *q, *kc, *vc;
   const int32_t *table, *seq_lens, *cu_new;
   float* part;
-  int4* rec;  // [kGrid]: a unit that begins in range b and ends in another one: first row, rows (0: none), head and part, last range
+  // [kGrid]: a unit that begins in range b and ends in another one: first row, rows, head and part, last range; or, where range
+  // b lies inside a unit: the range in which that begins, -1; or 0, 0
+  int4* rec;
   uint16_t* o;
   float* lse;
   int B, Hq, Hkv, G, GP, parts, T;  // GP: heads of a unit
@@ -139,7 +141,7 @@ struct Lds {
 };
 
 // A unit of the line and the range's tiles of it. I: the type of slots, 32 bits where they hold all of them (8 rows over 4K
-// tokens 21.8 us, with 64 bits 22.2).
+// tokens 19 us, with 64 bits 0.4 more).
 template <class I>
 struct Unit {
   ChunkSeq S;
@@ -741,6 +743,7 @@ void chunk_kernel(const ChunkParams P) {
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the buffer is free for this wave's next copy
     }
+    if (threadIdx.x == 0 && E.t0 > 0 && E.t1 < E.tiles) P.rec[b] = int4{(int)(E.at / (I)lds.range[2]), -1, 0, 0};
     if (threadIdx.x == 0 && E.t0 == 0 && !whole)
       P.rec[b] = int4{E.row0 + E.j * P.T, min(P.T, E.S.w - E.j * P.T) * heads_of(P, E.hp), E.g * P.parts + E.hp,
                       (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
@@ -750,42 +753,45 @@ void chunk_kernel(const ChunkParams P) {
 }
 
 constexpr int kJoinThreads = 512;
+// With 16, 8 rows over 4K tokens, 16 parts, take 22.2 us instead of 19.1; with 3, few workgroups join many rows one by one (16
+// rows over 1000 tokens 25 us instead of 16).
+constexpr int kFewParts = 8;
 
 // Joins the partial results of the unit that begins in range blockIdx.x and ends in another one, for 16 R of its rows: 32
-// lanes take R of them. Two where a call has many (128 rows over 4K tokens 53.6 us, 56.7 with one), one where the parts
-// are what is many (8 rows over 4K 21.8 us, 23.1 with two). Bound: the partial results once, 132 KB a unit's range, most of them
-// in the caches (3.4 us at least, 13.5 to 16 for the large calls' 68 MB).
+// lanes take R of them. Two where a call has many (128 rows over 4K tokens 41.8 us, 46.2 with one), one where the parts
+// are what is many (8 rows over 4K 18.8 us, 20.5 with two). Of a unit of more than kFewParts parts a workgroup takes a row at a
+// time, 32 lanes a sixteenth of its parts, and the workgroups of the ranges inside it take rows as well: 2 rows of 20 heads
+// over 49K tokens, 193 parts, 24 us instead of 90; 128 rows over 4K 42 instead of 54. Bound: the partial results once, 132 KB a
+// unit's range, most of them in the caches (3.4 us at least, 13.5 to 16 for the large calls' 68 MB).
 template <int R>
 __global__ __launch_bounds__(kJoinThreads) void chunk_join_kernel(const ChunkParams P) {
-  const int4 rec = P.rec[blockIdx.x];
-  const int x0 = blockIdx.y * (kJoinThreads / 32 * R) + (threadIdx.x >> 5), t = threadIdx.x & 31;
-  if (x0 >= rec.y) return;
-  constexpr int kStep = kJoinThreads / 32;
-  const int last = rec.y - 1;
-  int x[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) x[r] = min(x0 + r * kStep, last);
+  int4 rec = P.rec[blockIdx.x];
+  if (rec.y == 0) return;
+  const int first = rec.y < 0 ? rec.x : (int)blockIdx.x;
+  if (rec.y < 0) rec = P.rec[first];
+  const int n_parts = rec.w - first + 1;
   const size_t stride = (size_t)P.part_rows * kRowFloats;
-  const int n_parts = rec.w - (int)blockIdx.x + 1;
-  const auto part = [&](int i) { return P.part + ((size_t)(blockIdx.x + i) * 2 + (i == 0)) * stride; };
-  float M[R], L[R];
-  f32x4_t O[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    M[r] = -INFINITY;
-    L[r] = 0.f;
-    O[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  // N parts at a time, so that their loads wait side by side: two where there are no more, as in most long calls.
-  const auto add = [&](auto nc, int i0) __attribute__((always_inline)) {
-    constexpr int N = decltype(nc)::value;
-    float m[N][R], l[N][R];
-    f32x4_t o[N][R];
+  const auto part = [&](int i) { return P.part + ((size_t)(first + i) * 2 + (i == 0)) * stride; };
+  const int hp = rec.z % P.parts, heads = heads_of(P, hp), head0 = rec.z / P.parts * P.G + hp * P.GP;
+  const int group = threadIdx.x >> 5, t = threadIdx.x & 31;
+  const auto join = [&](float& M, float& L, f32x4_t& O, float m, float l, const f32x4_t& o) __attribute__((always_inline)) {
+    const float mx = fmaxf(M, m), base = mx == -INFINITY ? 0.f : mx;
+    const float a = __builtin_amdgcn_exp2f((M - base) * P.scale_log2);
+    const float c = __builtin_amdgcn_exp2f((m - base) * P.scale_log2);
+    L = a * L + c * l;
+    O = a * O + c * o;
+    M = mx;
+  };
+  // Parts i0, i0 + step ... to rows x: N of them at a time, so that their loads wait side by side.
+  const auto add = [&](auto nc, auto rc, const int* x, int i0, int step, float* M, float* L, f32x4_t* O) __attribute__((always_inline)) {
+    constexpr int N = decltype(nc)::value, RR = decltype(rc)::value;
+    float m[N][RR], l[N][RR];
+    f32x4_t o[N][RR];
 #pragma unroll
     for (int i = 0; i < N; ++i) {  // behind the last part: that one again, without weight
-      const float* p = part(min(i0 + i, n_parts - 1));
+      const float* p = part(min(i0 + i * step, n_parts - 1));
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
+      for (int r = 0; r < RR; ++r) {
         m[i][r] = p[(size_t)P.part_rows * kHeadDim + x[r]];
         l[i][r] = p[(size_t)P.part_rows * (kHeadDim + 1) + x[r]];
         o[i][r] = *reinterpret_cast<const f32x4_t*>(p + (size_t)x[r] * kHeadDim + t * 4);
@@ -793,34 +799,69 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join_kernel(const ChunkPar
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (i0 + i >= n_parts) break;
+      if (i0 + i * step >= n_parts) break;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const float mx = fmaxf(M[r], m[i][r]), base = mx == -INFINITY ? 0.f : mx;
-        const float a = __builtin_amdgcn_exp2f((M[r] - base) * P.scale_log2);
-        const float c = __builtin_amdgcn_exp2f((m[i][r] - base) * P.scale_log2);
-        L[r] = a * L[r] + c * l[i][r];
-        O[r] = a * O[r] + c * o[i][r];
-        M[r] = mx;
-      }
+      for (int r = 0; r < RR; ++r) join(M[r], L[r], O[r], m[i][r], l[i][r], o[i][r]);
     }
   };
-  if (n_parts <= 2) add(std::integral_constant<int, 2>{}, 0);
-  else
-    for (int i0 = 0; i0 < n_parts; i0 += 8) add(std::integral_constant<int, 8>{}, i0);
-  const int hp = rec.z % P.parts, heads = heads_of(P, hp), head0 = rec.z / P.parts * P.G + hp * P.GP;
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (x0 + r * kStep > last) break;
-    const int tok = x[r] / heads;
-    const size_t out = (size_t)(rec.x + tok) * P.Hq + head0 + (x[r] - tok * heads);
-    const bool none = L[r] == 0.f;
+  const auto write = [&](int x, float M, float L, const f32x4_t& O) __attribute__((always_inline)) {
+    const int tok = x / heads;
+    const size_t out = (size_t)(rec.x + tok) * P.Hq + head0 + (x - tok * heads);
+    const bool none = L == 0.f;
     float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : O[r][e] / L[r];
+    for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : O[e] / L;
     store4(P.o + out * kHeadDim + t * 4, v);
-    if (P.lse && t == 0) P.lse[out] = none ? -INFINITY : M[r] * P.scale + logf(L[r]);
+    if (P.lse && t == 0) P.lse[out] = none ? -INFINITY : M * P.scale + logf(L);
+  };
+  constexpr int kStep = kJoinThreads / 32;
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
+  const std::integral_constant<int, 8> eight;
+  if (n_parts > kFewParts) {
+    __shared__ f32x4_t sums[kStep][32];
+    __shared__ float tops[kStep], totals[kStep];
+    const int workers = (rec.w - first) * gridDim.y;
+    for (int x = (blockIdx.x - first) * gridDim.y + blockIdx.y; x < rec.y; x += workers) {
+      float M = -INFINITY, L = 0.f;
+      f32x4_t O = {0.f, 0.f, 0.f, 0.f};
+      if (n_parts <= 2 * kStep) add(two, one, &x, group, kStep, &M, &L, &O);
+      else
+        for (int i0 = group; i0 < n_parts; i0 += 8 * kStep) add(eight, one, &x, i0, kStep, &M, &L, &O);
+      sums[group][t] = O;
+      if (t == 0) {
+        tops[group] = M;
+        totals[group] = L;
+      }
+      __syncthreads();
+      if (group == 0) {
+#pragma unroll
+        for (int i = 1; i < kStep; ++i) join(M, L, O, tops[i], totals[i], sums[i][t]);
+        write(x, M, L, O);
+      }
+      __syncthreads();
+    }
+    return;
   }
+  const int x0 = blockIdx.y * (kStep * R) + group, last = rec.y - 1;
+  if (first != (int)blockIdx.x || x0 > last) return;
+  int x[R];
+  float M[R], L[R];
+  f32x4_t O[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    x[r] = min(x0 + r * kStep, last);
+    M[r] = -INFINITY;
+    L[r] = 0.f;
+    O[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const std::integral_constant<int, R> rows;
+  if (n_parts <= 2) add(two, rows, x, 0, 1, M, L, O);
+  else
+    for (int i0 = 0; i0 < n_parts; i0 += 8) add(eight, rows, x, i0, 1, M, L, O);
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (x0 + r * kStep <= last) write(x[r], M[r], L[r], O[r]);
 }
 
 // Rows of a partial result: those that a unit can have.

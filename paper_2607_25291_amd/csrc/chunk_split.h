@@ -16,7 +16,7 @@ constexpr int kChunkRows = 256;  // rows of a unit
 constexpr int kChunkTile = 128;  // keys of a tile
 // Slots of a key in a unit, and in one whose rows leave half of the workgroup idle (its tiles take some 5,000 cycles, others
 // 7,000). Counted alike, the ranges of one-token units end early: 48 sequences of which 43 add one token 828 us instead of
-// 791, 8 rows over 4K tokens 24.6 instead of 21.8.
+// 791.
 constexpr int kFullSlots = 3, kFewSlots = 2;
 // What taking up a unit costs beside its keys, in keys; at least a tile, so that a unit's last tile starts inside its
 // slots. 19 prompts of up to 4K tokens with 192 / 320 / 448 / 640 keys: 927 / 781 / 723 / 742 us (prefetches across units are

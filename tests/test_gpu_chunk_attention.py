@@ -70,3 +70,15 @@ def test_rows_in_front_of_token_0_see_nothing():
     _, _, _, cu, o, ls = one(4, 4, 2, 16, [10, 0, 300], [200, 70, 310])
     assert (as_f64(o)[:190] == 0).all() and np.isneginf(ls.cpu().numpy()[:190]).all()
     assert (as_f64(o)[200:270] == 0).all()
+
+
+@pytest.mark.parametrize("length", [256, 257, 2048, 2049, 8192, 8193])
+def test_units_of_so_many_parts(length):
+    """One unit in 1, 2, 8, 9, 32 and 33 ranges; its rows are shared out among their workgroups from 9 on."""
+    one(5, 4, 1, 64, [length], [3])
+
+
+def test_many_rows_of_many_parts():
+    one(6, 4, 1, 32, [12000], [64])
+    one(7, 10, 2, 32, [300, 7000], [2, 50])
+    one(8, 300, 1, 16, [3000], [2])
