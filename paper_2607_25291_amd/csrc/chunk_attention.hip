@@ -19,8 +19,8 @@
 // Bound: MFMA, 4 d flops a key and row. 4096 tokens over 64K, 32 / 8 heads: 3.8 to 3.9 ms, 1.10 PFLOP/s of 1.23 in a library
 // matrix product of 8192 rows; 0.57 of the cycles multiply at 1.77 GHz, LDS bank conflicts are below 0.1 %. 256 rows: eight
 // waves share a tile's copies, and two waves a SIMD, one phase apart, let one multiply while the other one takes
-// exponentials. What a unit costs beside its tiles (3.5 tiles: Q, edges, results) leaves 840 TFLOP/s in prompts of up to 4K
-// tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64 sequences of up to 64K tokens and one new
+// exponentials. What a unit costs beside its tiles (3 tiles: edges, results, a side that waits for the other one's) leaves 860
+// TFLOP/s in prompts of up to 4K tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64 sequences of up to 64K tokens and one new
 // token 287 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 us) are two launches and latency.
 #include <float.h>
 #include <limits.h>
@@ -134,7 +134,8 @@ __device__ __forceinline__ void end_phase(bool full) {
 struct Lds {
   char v[2][kTileBytes];  // the low 64 KiB: every transposing read's offsets fit its immediate
   char k[2][kTileBytes];
-  int32_t unit[kWaves][2][16];  // a wave's unit and its next one
+  int32_t unit[4][4][16];  // units in turn, a copy for the two waves of a SIMD: side 0 writes them
+  int32_t pages[4][2][64]; // of the next unit's first tiles: a wave's two runs, a tile each
   int64_t range[3];             // the range's first slot and its end, and the length of all ranges
   int row[kChunkRows];  // token and head of a row, for units of GP heads: token << 16 | head
   int odd[2][4];        // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
@@ -150,7 +151,7 @@ struct Unit {
   I at;         // its first slot
   int tiles, t0, t1;
 };
-// Units wait in LDS, one copy a wave: in scalar registers, two of them would push other values out.
+// Units wait in LDS: in scalar registers, two of them would push other values out.
 template <class I>
 __device__ __forceinline__ void put(int32_t* to, const Unit<I>& u) {
   if ((threadIdx.x & 63) == 0) {
@@ -340,16 +341,14 @@ void chunk_kernel(const ChunkParams P) {
   };
   // Physical pages of the runs of tiles t .. t + 63, one tile a lane (run r: rows 32 wl + 16 r).
   // Behind the last key the last entry is read again (no branch in which lanes part: what follows stays uniform).
+  const auto page_of = [&](const int32_t* row, int keys, int t, int r) __attribute__((always_inline)) -> int {
+    if (keys <= 0) return 0;
+    const int64_t x = (int64_t)(t + again(lane)) * kTile + wl * 32 + r * 16;
+    return row[min(x, (int64_t)keys - 1) >> P.log2_page];
+  };
   const auto look_up = [&](int t) __attribute__((always_inline)) {
-    const int ln = again(lane);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      pg[r] = 0;
-      if (f_keys > 0) {
-        const int64_t x = (int64_t)(t + ln) * kTile + wl * 32 + r * 16;
-        pg[r] = f_row[min(x, (int64_t)f_keys - 1) >> P.log2_page];
-      }
-    }
+    for (int r = 0; r < 2; ++r) pg[r] = page_of(f_row, f_keys, t, r);
   };
   const auto copy = [&](int t, int i, int buf) __attribute__((always_inline)) {
     char* dst = (side ? lds.v[0] : lds.k[0]) + buf * kTileBytes + wl * 32 * 256;
@@ -436,7 +435,25 @@ void chunk_kernel(const ChunkParams P) {
     for (int c = 0; c < 8; ++c) qf[c] = as_bf16x8(ldg16(qp + 16 * c));
   };
 
+  // Side 0: the unit behind that in place `slot`, and its first pages, for both sides. A range's last unit has one of no tiles
+  // behind it. In front of a unit's tiles: looked for at its last tile by either side, the next unit held up the barrier by
+  // 5,000 cycles a side (19 prompts 774 us, now 757), and inside the loop over the tiles that code slows the loop down (4K tokens over 64K
+  // 3.92 ms, now 3.86).
+  int slot = 0;
+  const auto prepare = [&]() __attribute__((always_inline)) {
+    Unit<I> N = get<I>(lds.unit[wl][slot & 3], P);
+    if (!advance(N, uniform((I)lds.range[0]), uniform((I)lds.range[1]))) N.t1 = 0;
+    put(lds.unit[wl][(slot + 1) & 3], N);
+    if (N.t1 == 0) return;
+    int e[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) e[r] = page_of(P.table + (size_t)N.n * P.max_pages, uniform(N.S.keys(N.j)), 0, r);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) lds.pages[wl][r][again(lane)] = e[r];
+  };
+
   int buf = 0;
+  if (side == 0) put(lds.unit[wl][0], D);
   fetch_from(D);
   look_up(D.t0);
   load_q(D);
@@ -445,10 +462,8 @@ void chunk_kernel(const ChunkParams P) {
   end_phase(true);
   if (side == 1) end_phase(false);
 
-  int parity = 0;
-  put(lds.unit[w][0], D);
-  for (;;) {
-    const Unit<I> D = get<I>(lds.unit[w][parity], P);
+  for (;; ++slot) {
+    const Unit<I> D = get<I>(lds.unit[wl][slot & 3], P);
     const bool live = w * 32 < min(P.T, D.S.w - D.j * P.T) * heads_of(P, D.hp);
     const int pos_low = uniform(pos);  // of the wave's rows
     const int pos_top = __builtin_amdgcn_readlane(pos, 31);
@@ -608,20 +623,21 @@ void chunk_kernel(const ChunkParams P) {
     bool more = false;
     int i = 0;  // tiles behind the last look_up
     const int t1 = D.t1;
+    if (side == 0) prepare();
     int t_end = t1;
     asm volatile("" : "+s"(t_end));  // a loop of its own: `last` is not taken for its exit
     for (int t = D.t0; t < t_end; ++t) {
       const bool last = t + 1 == t1;
       int to = t + 1;
       if (last) {
-        Unit<I> N = get<I>(lds.unit[w][parity], P);
-        more = uniform((int)advance(N, uniform((I)lds.range[0]), uniform((I)lds.range[1])));
+        const Unit<I> N = get<I>(lds.unit[wl][(slot + 1) & 3], P);
+        more = N.t1 != 0;
         i = 0;
         to = 0;
         if (more) {
-          put(lds.unit[w][parity ^ 1], N);
           fetch_from(N);
-          look_up(0);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) pg[r] = lds.pages[wl][r][again(lane)];
         }
       } else if (++i == 64) {
         look_up(to);
@@ -630,7 +646,7 @@ void chunk_kernel(const ChunkParams P) {
       const bool fetch = !last || more;
       Logits X;
       qk_half(t, X);
-      if (last && more) load_q(get<I>(lds.unit[w][parity ^ 1], P));  // its registers are free from here on
+      if (last && more) load_q(get<I>(lds.unit[wl][(slot + 1) & 3], P));  // its registers are free from here on
       if (fetch) copy(to, i, buf ^ 1);
       end_phase(false);
       if (first_pos - t * kTile < kTile - 1) {
@@ -644,7 +660,7 @@ void chunk_kernel(const ChunkParams P) {
     }
 
     if (!more && side == 0) end_phase(false);  // as many barriers on both sides; side 1 need not wait for these results
-    const Unit<I> E = get<I>(lds.unit[w][parity], P);
+    const Unit<I> E = get<I>(lds.unit[wl][slot & 3], P);
     const bool whole = E.t0 == 0 && E.t1 == E.tiles;
     if (live) {
       // Results go to memory in whole rows, through the part of the tile that this wave moves, in the buffer of the unit's last
@@ -748,7 +764,6 @@ void chunk_kernel(const ChunkParams P) {
       P.rec[b] = int4{E.row0 + E.j * P.T, min(P.T, E.S.w - E.j * P.T) * heads_of(P, E.hp), E.g * P.parts + E.hp,
                       (int)((E.at + (I)(E.tiles - 1) * kChunkTile * E.S.key_slots(E.j)) / (I)lds.range[2])};
     if (!more) break;
-    parity ^= 1;
   }
 }
 

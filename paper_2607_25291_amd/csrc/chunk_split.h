@@ -19,9 +19,9 @@ constexpr int kChunkTile = 128;  // keys of a tile
 // 791.
 constexpr int kFullSlots = 3, kFewSlots = 2;
 // What taking up a unit costs beside its keys, in keys; at least a tile, so that a unit's last tile starts inside its
-// slots. 19 prompts of up to 4K tokens with 192 / 320 / 448 / 640 keys: 927 / 781 / 723 / 742 us (prefetches across units are
-// in these); with 448 the ranges end within 3 % of each other.
-constexpr int kUnitKeys = 448;
+// slots. 19 prompts of up to 4K tokens with 288 / 352 / 400 / 448 keys: 787 / 767 / 757 / 767 us; the ranges end within 5 % of
+// each other.
+constexpr int kUnitKeys = 400;
 
 // Heads of a unit, units that share a group, and tokens of a unit, for G query heads per KV head.
 constexpr int chunk_heads(int G) { return G < kChunkRows ? G : kChunkRows; }
