@@ -19,9 +19,10 @@
 // Bound: MFMA, 4 d flops a key and row. 4096 tokens over 64K, 32 / 8 heads: 3.8 to 3.9 ms, 1.10 PFLOP/s of 1.23 in a library
 // matrix product of 8192 rows; 0.57 of the cycles multiply at 1.77 GHz, LDS bank conflicts are below 0.1 %. 256 rows: eight
 // waves share a tile's copies, and two waves a SIMD, one phase apart, let one multiply while the other one takes
-// exponentials. What a unit costs beside its tiles (3 tiles: edges, results, a side that waits for the other one's) leaves 820
-// to 860 TFLOP/s in prompts of up to 4K tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64 sequences of up to 64K tokens and one new
-// token 287 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 us) are two launches and latency.
+// exponentials. What a unit costs beside its tiles (3 tiles: edges, results, a side that waits for the other one's) leaves
+// 820 to 860 TFLOP/s in prompts of up to 4K tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64
+// sequences of up to 64K tokens and one new token 287 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 to
+// 15.8 us) are two launches and latency.
 #include <float.h>
 #include <limits.h>
 
