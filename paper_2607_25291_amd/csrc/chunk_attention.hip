@@ -880,10 +880,14 @@ __global__ __launch_bounds__(kJoinThreads) void chunk_join_kernel(const ChunkPar
     if (x0 + r * kStep <= last) write(x[r], M[r], L[r], O[r]);
 }
 
-// Rows of a partial result: those that a unit can have.
+// Rows of a partial result: those that a unit can have, an even number, so that every partial result starts at a multiple of 16
+// bytes, which the vector loads and stores of O take for granted.
 int part_rows(const ChunkShape& sh) {
-  return (int)std::min<long long>(kChunkRows, (long long)std::min(sh.n_rows, chunk_tokens(sh.G)) * chunk_heads(sh.G));
+  const long long rows = std::min<long long>(kChunkRows, (long long)std::min(sh.n_rows, chunk_tokens(sh.G)) * chunk_heads(sh.G));
+  return (int)(rows + rows % 2);
 }
+static_assert(2 * kRowFloats * sizeof(float) % 16 == 0 && kChunkRows % 2 == 0 && kGrid * sizeof(int4) % 16 == 0,
+              "partial results lie at multiples of 16 bytes");
 
 }  // namespace
 
