@@ -25,6 +25,7 @@
 // 15.8 us) are two launches and latency.
 #include <float.h>
 #include <limits.h>
+#include <stddef.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -139,8 +140,11 @@ struct Lds {
   int32_t pages[4][2][64]; // of the next unit's first tiles: a wave's two runs, a tile each
   int64_t range[3];             // the range's first slot and its end, and the length of all ranges
   int row[kChunkRows];  // token and head of a row, for units of GP heads: token << 16 | head
-  int odd[2][4];        // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
+  alignas(16) int odd[2][4];  // whether a wave's part of the V tile holds an infinite or NaN value (tiles that not all rows see)
 };
+static_assert(offsetof(Lds, v) % 1024 == 0 && offsetof(Lds, k) % 1024 == 0 && offsetof(Lds, unit) % 16 == 0 &&
+                  offsetof(Lds, range) % 8 == 0 && offsetof(Lds, odd) % 16 == 0,
+              "what is read and written 16 bytes at a time lies at multiples of 16 bytes");
 
 // A unit of the line and the range's tiles of it. I: the type of slots, 32 bits where they hold all of them (8 rows over 4K
 // tokens 19 us, with 64 bits 0.4 more).
