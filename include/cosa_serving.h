@@ -61,7 +61,8 @@ typedef struct {
  * seq_lens is read as clamped to [0, max_pages * page_size], cu_new to [0, n_rows], a sequence that ends in front of
  * its start as empty; sequences whose rows overlap leave one of their results in them. A request that cosa_page_map left
  * out has rows in cu_new but no new tokens: they count as its last cached ones. Table entries outside [0, n_pages) are
- * read as page 0. The workspace is scratch of at least cosa_chunk_workspace_bytes() bytes, 16-byte aligned.
+ * read as page 0. The workspace is scratch of at least cosa_chunk_workspace_bytes() bytes, 16-byte aligned. o, lse and the
+ * workspace overlap neither the inputs, the caches' n_pages pages among them, nor each other.
  */
 size_t cosa_chunk_workspace_bytes(const cosa_chunk_problem* problem);
 cosa_status cosa_chunk_attention(const cosa_chunk_problem* problem, const void* q,

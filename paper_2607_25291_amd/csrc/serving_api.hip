@@ -122,13 +122,15 @@ cosa_status cosa_chunk_attention(const cosa_chunk_problem* problem, const void* 
   for (const void* p : {(const void*)kv->k_cache, (const void*)kv->v_cache, q, (const void*)o})
     if (misaligned(p, 16)) return fail(COSA_ERR_INVALID_ARG, "k_cache, v_cache, q and o must be 16-byte aligned");
   if ((st = check_workspace(workspace, workspace_bytes, cosa::chunk_workspace_bytes(sh))) != COSA_OK) return st;
+  // Other workgroups read all inputs until the call's end.
   const int64_t row = 2ll * sh.Hq * cosa::kHeadDim;
-  const Span queries{q, 2 * (sh.n_rows - 1) * sh.q_stride + row}, out{o, sh.n_rows * row},
-      sums{lse, 4ll * sh.n_rows * sh.Hq}, scratch{workspace, (int64_t)cosa::chunk_workspace_bytes(sh)};
-  if (out.meets(queries) || sums.meets(queries) || scratch.meets(queries))
-    return fail(COSA_ERR_INVALID_ARG, "o, lse and the workspace must not overlap q");
-  if (out.meets(sums) || out.meets(scratch) || sums.meets(scratch))
-    return fail(COSA_ERR_INVALID_ARG, "o, lse and the workspace must not overlap each other");
+  const double pages = 2.0 * cosa::kHeadDim * sh.n_pages * sh.Hkv * kv->page_size;
+  const int64_t cache = pages < 1e18 ? 2ll * cosa::kHeadDim * sh.n_pages * sh.Hkv * kv->page_size : (int64_t)1e18;
+  const Span in[] = {{q, 2 * (sh.n_rows - 1) * sh.q_stride + row}, {kv->k_cache, cache}, {kv->v_cache, cache},
+                     {kv->page_table, 4ll * sh.B * sh.max_pages}, {seq_lens, 4ll * sh.B}, {cu_new, 4ll * (sh.B + 1)}};
+  const Span out[] = {{o, sh.n_rows * row}, {lse, 4ll * sh.n_rows * sh.Hq},
+                      {workspace, (int64_t)cosa::chunk_workspace_bytes(sh)}};
+  if ((st = check_apart(out, in, "o, lse and the workspace")) != COSA_OK) return st;
   const cosa::ChunkArgs a{u16(q), u16(kv->k_cache), u16(kv->v_cache), kv->page_table, seq_lens, cu_new, workspace,
                           static_cast<uint16_t*>(o), lse};
   return launch(stream, "chunk_attention launch",
