@@ -55,8 +55,9 @@ typedef struct {
  * where all its logits are -inf. Rows of no sequence are not written.
  * fp32 logits, softmax and sums; probabilities are rounded to bf16 for the product with V, as in the prefill. What
  * the cache holds behind seq_lens, and behind p for one row, does not matter, NaN and infinities included. An
- * infinite v[t] that is seen gives that infinity in its element (NaN beside one of the other sign, or where its
- * weight is 0 or below 2^-100 of the largest); NaN values and logits that are seen give NaN.
+ * infinite v[t] that is seen gives that infinity in its element: NaN beside one of the other sign or where its logit
+ * is -inf (a weight of 0), either of the two where its weight is below 2^-100 of the largest. NaN values and logits that
+ * are seen give NaN.
  * The keys are split over a fixed grid and joined in a fixed order: results are deterministic.
  * seq_lens is read as clamped to [0, max_pages * page_size], cu_new to [0, n_rows], a sequence that ends in front of
  * its start as empty; sequences whose rows overlap leave one of their results in them. A request that cosa_page_map left

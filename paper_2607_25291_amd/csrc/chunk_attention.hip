@@ -25,6 +25,7 @@
 // 15.8 us) are two launches and latency.
 #include <float.h>
 #include <limits.h>
+#include <math.h>
 #include <stddef.h>
 
 #include <algorithm>
@@ -678,7 +679,8 @@ void chunk_kernel(const ChunkParams P) {
       char* mine_row = stage + r32 * 256;
       const int n_real = __builtin_popcountll(__ballot(real)) / 2;  // rows of the wave, the first ones
       const int r4 = ln >> 4, slot = ln & 15;  // of rows 4 i + r4
-      // The values that were taken as 0, to the staged rows that see them: elements d0 .. d0 + n - 1, T each.
+      // The values that were taken as 0, to the staged rows that see them: elements d0 .. d0 + n - 1, T each. Where the row's
+      // logit is -inf, the value's weight is 0, and their product is NaN, as it is in the tiles that all rows see.
       const auto add_odd = [&](auto type, int d0, int n, bool none) __attribute__((always_inline)) {
         using V = decltype(type);
         const int32_t* trow = P.table + (size_t)E.n * P.max_pages;
@@ -687,14 +689,24 @@ void chunk_kernel(const ChunkParams P) {
         for (int t = odd_from; t <= to; ++t) {
           const int32_t e = ld_uniform(trow + (t >> P.log2_page));
           const uint64_t p = (uint32_t)e < (uint64_t)P.n_pages ? (uint32_t)e : 0u;
-          const uint16_t* v = P.vc + (p * page_bytes + (uint64_t)E.g * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim;
+          const size_t at = uniform((int64_t)((p * page_bytes + (uint64_t)E.g * head_bytes) / 2 + (size_t)(t & page_mask) * kHeadDim));
+          const uint32_t two = reinterpret_cast<const uint32_t*>(P.vc + at)[again(lane)];
+          if (!__any((two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u)) continue;
+          const uint16_t* qp = P.q + (size_t)(E.row0 + tok) * P.q_stride + (size_t)head * kHeadDim;
+          float logit = 0.f;
 #pragma unroll 1
-          for (int i = hf * (n / 2); i < (hf + 1) * (n / 2); ++i) {
-            const uint32_t bits = (uint32_t)v[d0 + i] << 16;
-            if ((bits & 0x7f800000u) != 0x7f800000u || t > E.S.len - E.S.w + tok || none) continue;
-            const int byte = i * (int)sizeof(V);
-            V* x = reinterpret_cast<V*>(mine_row + (((byte >> 4) ^ (r32 & 15)) << 4) + (byte & 15));
-            *x = (V)((float)*x + __uint_as_float(bits));
+          for (int c = 0; c < kHeadDim; ++c)
+            logit = fmaf(__uint_as_float((uint32_t)qp[c] << 16), __uint_as_float((uint32_t)P.kc[at + c] << 16), logit);
+          if (t <= E.S.len - E.S.w + tok && !none) {
+#pragma unroll 1
+            for (int i = again(hf) * (n / 2), i1 = i + n / 2; i < i1; ++i) {
+              const uint32_t bits = (uint32_t)P.vc[at + d0 + i] << 16;
+              if ((bits & 0x7f800000u) == 0x7f800000u) {
+                const int byte = i * (int)sizeof(V);
+                V* x = reinterpret_cast<V*>(mine_row + (((byte >> 4) ^ (r32 & 15)) << 4) + (byte & 15));
+                *x = (V)((float)*x + (logit == -INFINITY ? NAN : __uint_as_float(bits)));
+              }
+            }
           }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
