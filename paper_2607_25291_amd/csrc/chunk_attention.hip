@@ -96,6 +96,27 @@ __device__ __forceinline__ ChunkSeq seq_of_uniform(const ChunkParams& P, int n, 
   return {uniform(S.len), uniform(S.w), P.T, P.GP};
 }
 
+// The first sequence from n on that has rows; P.B if none has. 256 at a time, four a lane: one by one, a batch of 512 / 8192 slots
+// of which the first and the last are busy takes 68 / 868 us, now 17 / 28 (16.6 / 19.7 where they lie side by side).
+__device__ __forceinline__ int next_with_rows(const ChunkParams& P, int n) {
+  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  for (; n < P.B; n += 4 * 64) {
+    int32_t from[4], to[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = min(n + 64 * k + lane, P.B - 1);  // behind the last one: that one again, which its own lane finds first
+      from[k] = P.cu_new[i];
+      to[k] = P.cu_new[i + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint64_t busy = __ballot(min(to[k], P.n_rows) > max(from[k], 0));
+      if (busy) return uniform(n + 64 * k + (int)__builtin_ctzll(busy));
+    }
+  }
+  return P.B;
+}
+
 // Heads of unit part hp of a group.
 __device__ __forceinline__ int heads_of(const ChunkParams& P, int hp) { return min(P.G - hp * P.GP, P.GP); }
 
@@ -312,10 +333,13 @@ void chunk_kernel(const ChunkParams P) {
       }
       if (u.g == P.Hkv) {
         u.g = 0;
-        do {  // there are slots left, so there is another sequence with rows
-          if (++u.n >= P.B) return false;
+        if (++u.n >= P.B) return false;
+        u.S = seq_of_uniform(P, u.n, u.row0);
+        if (u.S.w == 0) {  // there are slots left, so there is another sequence with rows
+          u.n = next_with_rows(P, u.n + 1);
+          if (u.n >= P.B) return false;
           u.S = seq_of_uniform(P, u.n, u.row0);
-        } while (u.S.w == 0);
+        }
       }
     }
     settle(u, begin, end);
