@@ -53,14 +53,17 @@ typedef struct {
  * q [n_rows, Hq, d] (q_stride between rows), o [n_rows, Hq, d] dense, bf16; lse (NULL to omit) fp32 [n_rows, Hq]: the
  * natural logarithm of the softmax's sum of exponentials. A row with p < 0 sees nothing: o = 0 and lse = -inf, as
  * where all its logits are -inf. Rows of no sequence are not written.
- * fp32 logits, softmax and sums; probabilities are rounded to bf16 for the product with V, as in the prefill. What
+ * fp32 logits, softmax and sums; probabilities are rounded to bf16 for the product with V, as in the prefill (those of
+ * cosa_decode_attention keep 32 bits). What
  * the cache holds behind seq_lens, and behind p for one row, does not matter, NaN and infinities included. An
  * infinite v[t] that is seen gives that infinity in its element: NaN beside one of the other sign or where its logit
  * is -inf (a weight of 0), either of the two where its weight is below 2^-100 of the largest. NaN values and logits that
  * are seen give NaN.
- * The keys are split over a fixed grid and joined in a fixed order: results are deterministic.
+ * The keys are split over a fixed grid and joined in a fixed order: results are deterministic where no row belongs to
+ * several sequences.
  * seq_lens is read as clamped to [0, max_pages * page_size], cu_new to [0, n_rows], a sequence that ends in front of
- * its start as empty; sequences whose rows overlap leave one of their results in them. A request that cosa_page_map left
+ * its start as empty; rows of several sequences (offsets that fall) hold parts of any of their results, and not the same
+ * ones every time. A request that cosa_page_map left
  * out has rows in cu_new but no new tokens: they count as its last cached ones. Table entries outside [0, n_pages) are
  * read as page 0. The workspace is scratch of at least cosa_chunk_workspace_bytes() bytes, 16-byte aligned. o, lse and the
  * workspace overlap neither the inputs, the caches' n_pages pages among them, nor each other.

@@ -13,16 +13,18 @@
 // kernel joins in order.
 //
 // o = sum_t exp(s_t - M) v_t / sum_t exp(s_t - M), in one pass: where a larger maximum comes, what is summed so far is
-// multiplied by exp(old - new). Weights are rounded to bf16 for the product with V, as in the prefill (2^-8 of a weight;
-// their sum takes them with 24 bits): the further bits would be products of their own, and MFMA is what bounds large units.
+// multiplied by exp(old - new). Weights are rounded to bf16 for the product with V, as in the prefill (at most half a step, 2^-8,
+// of a weight; their sum takes them with 24 bits): the further bits would be products of their own, and MFMA is what bounds large
+// units. Units of few rows, which memory bounds, round alike: a token's weights do not depend on what shares its unit. The
+// results' error against 64 bits grows by 0.5 to 2 % over that of their last rounding to bf16 (1.65e-3 to 1.68e-3, 19 prompts).
 //
-// Bound: MFMA, 4 d flops a key and row. 4096 tokens over 64K, 32 / 8 heads: 3.8 to 3.9 ms, 1.10 PFLOP/s of 1.23 in a library
-// matrix product of 8192 rows; 0.57 of the cycles multiply at 1.77 GHz, LDS bank conflicts are below 0.1 %. 256 rows: eight
+// Bound: MFMA, 4 d flops a key and row. 4096 tokens over 64K, 32 / 8 heads: 3.7 to 3.9 ms, 1.13 PFLOP/s where a library matrix
+// product of 8192 rows takes 1.24; 0.59 of the cycles multiply at 1.78 GHz, LDS bank conflicts are below 0.1 %. 256 rows: eight
 // waves share a tile's copies, and two waves a SIMD, one phase apart, let one multiply while the other one takes
 // exponentials. What a unit costs beside its tiles (3 tiles: edges, results, a side that waits for the other one's) leaves
-// 820 to 860 TFLOP/s in prompts of up to 4K tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.7 TB/s (64
-// sequences of up to 64K tokens and one new token 287 us). The smallest calls (16 new ones of 300 tokens, 4 heads, 14.5 to
-// 15.8 us) are two launches and latency.
+// 840 to 880 TFLOP/s in prompts of up to 4K tokens. Units of few rows wait for the 64 KiB of one tile at a time: 5.6 TB/s (64
+// sequences of up to 64K tokens and one new token 292 us). The smallest calls (16 new ones of 1000 tokens, 4 heads, 16 us) are
+// two launches and latency.
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -43,8 +45,8 @@ constexpr int kTile = kChunkTile;
 constexpr int kKeyTiles = kTile / 32;
 constexpr int kTileBytes = kTile * kHeadDim * 2;  // one tensor's
 constexpr int kLog2Grid = 8, kGrid = 1 << kLog2Grid;  // workgroups that share the line: one a CU
-// Slots of the shortest range: at least a tile's. Shorter ones end sooner and leave more to join: 384 / 512 slots 17.8 / 18.8 us
-// for 8 rows over 4K tokens, 16.2 / 15.9 for 16 over 1000 and 26.3 / 24.0 for 2 rows of 20 heads over 49K.
+// Slots of the shortest range: at least a tile's. Shorter ones end sooner and leave more to join: 384 / 512 slots 18.1 / 19.4 us
+// for 8 rows over 4K tokens, 16.4 / 16.1 for 16 over 1000 and 26.2 / 24.0 for 2 rows of 20 heads over 49K; 0.5 % for 512 over 8K.
 constexpr int kShortest = 512;
 static_assert(kShortest >= kTile * kFullSlots, "every range but the last holds the start of a tile");
 constexpr int kRowFloats = kHeadDim + 2;          // of a partial result: O, maximum, sum
@@ -809,8 +811,8 @@ void chunk_kernel(const ChunkParams P) {
 }
 
 constexpr int kJoinThreads = 512;
-// With 16, 8 rows over 4K tokens, 16 parts, take 22.2 us instead of 19.1; with 3, few workgroups join many rows one by one (16
-// rows over 1000 tokens 25 us instead of 16).
+// With 16, 8 rows over 4K tokens, 16 parts, take 22.4 us instead of 19.4, and 128 rows 53 instead of 42; with 3, few workgroups
+// join many rows one by one (16 rows over 1000 tokens 25 us instead of 16, 512 over 8K 120 instead of 94).
 constexpr int kFewParts = 8;
 
 // Joins the partial results of the unit that begins in range blockIdx.x and ends in another one, for 16 R of its rows: 32
@@ -818,7 +820,7 @@ constexpr int kFewParts = 8;
 // are what is many (8 rows over 4K 18.8 us, 20.5 with two). Of a unit of more than kFewParts parts a workgroup takes a row at a
 // time, 32 lanes a sixteenth of its parts, and the workgroups of the ranges inside it take rows as well: 2 rows of 20 heads
 // over 49K tokens, 193 parts, 24 us instead of 90; 128 rows over 4K 42 instead of 54. Bound: the partial results once, 132 KB a
-// unit's range, most of them in the caches (3.4 us at least, 13.5 to 16 for the large calls' 68 MB).
+// unit's range, most of them in the caches (2.7 to 4.0 us for the smallest calls, 14 to 17 for the large ones' 68 MB).
 template <int R>
 __global__ __launch_bounds__(kJoinThreads) void chunk_join_kernel(const ChunkParams P) {
   int4 rec = P.rec[blockIdx.x];

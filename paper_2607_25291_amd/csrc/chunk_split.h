@@ -15,12 +15,13 @@ namespace cosa {
 constexpr int kChunkRows = 256;  // rows of a unit
 constexpr int kChunkTile = 128;  // keys of a tile
 // Slots of a key in a unit, and in one whose rows leave half of the workgroup idle (its tiles take some 5,000 cycles, others
-// 7,000). Counted alike, the ranges of one-token units end early: 48 sequences of which 43 add one token 828 us instead of
-// 791.
+// 7,000). Counted alike, the ranges of one-token units end early: 48 sequences of which 43 add one token 777 us instead of
+// 769 with 32 / 8 heads, 813 instead of 786 with 40 / 8. Prompts, whose last units alone differ, do not change.
 constexpr int kFullSlots = 3, kFewSlots = 2;
 // What taking up a unit costs beside its keys, in keys; at least a tile, so that a unit's last tile starts inside its
-// slots. 19 prompts of up to 4K tokens with 288 / 352 / 400 / 448 keys: 787 / 767 / 757 / 767 us; the ranges end within 5 % of
-// each other.
+// slots. 19 prompts of up to 4K tokens with 288 / 352 / 400 / 448 / 512 keys: 741 / 719 / 706 / 707 / 715 us with 28 / 4 heads and
+// pages of 16, 826 / 802 / 796 / 797 / 803 with 32 / 8 and 128, 447 / 441 / 440 / 440 / 444 with 16 / 16 and 64; a prompt of 8K 545 / 522 /
+// 522 / 523 / 527: flat from 352 on.
 constexpr int kUnitKeys = 400;
 
 // Heads of a unit, units that share a group, and tokens of a unit, for G query heads per KV head.

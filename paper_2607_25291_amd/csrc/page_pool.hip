@@ -5,10 +5,11 @@
 // the marks as bits in LDS. Otherwise kernels one after the other, with the marks as bytes in the workspace (plain
 // stores: a page marked twice gets the same byte twice): clear, mark, count by blocks, write.
 //
-// Bound: few entries, latency (64 rows: release 6.4 us, compaction 11.6, of which the second walk over the table and its
-// dependent loads are half). Many: the marks' stores, one byte each at random places (591K entries of 512 rows: 10.5 of
-// release's 19 us; 559K: 11 of compaction's 34), then launches that wait for each other, 2 to 4 us each, and the
-// compaction's lists and tables, 8 and 12 us.
+// Bound: few entries, latency (64 rows: release 5.2 us, compaction 11.5, of which the second walk over the table and its
+// dependent loads are half). Many: the marks' stores, one byte each at random places (591K entries of 512 rows: 11.3 of
+// release's 19 us; 559K: 11.2 of compaction's 33), then launches that wait for each other, 2 to 4 us each, and the
+// compaction's lists and tables, 8.3 and 12.1 us. Large pools: all marks are cleared and read, and every block adds up the
+// counts of all (64 rows of 4096 pages in a pool of 2^24 / 2^26 / 2^28 pages: release 32 / 136 / 1274 us, compaction 53 / 234 / 2330).
 #include <algorithm>
 
 #include "cosa_device.h"
@@ -103,7 +104,7 @@ __device__ __forceinline__ void free_list(const PageReleaseArgs& A, int& taken, 
 }
 
 // The rows of both tables, or of the one that both are, whose entries are then read and marked once (512 rows, of which half
-// end, 18.9 us, as two tables 23.5).
+// end, 19 us, as two tables 22).
 struct ReleaseRow {
   const int32_t* entries;
   int was, is;  // entries held before and afterwards; 0 for a row that the other table has
